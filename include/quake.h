@@ -68,7 +68,7 @@
 extern "C" {
 #endif
 
-#define QUAKE_ABI_VERSION 5
+#define QUAKE_ABI_VERSION 6
 
 typedef enum {
   QUAKE_F32 = 0,  /* IEEE binary32 */
@@ -361,6 +361,148 @@ quake_status quake_linear_gelu(const void* x, const void* w, void* y, int64_t m,
 quake_status quake_attention(const void* q, const void* k, const void* vt, void* o, int64_t heads,
                              int64_t seq, int64_t dim, int64_t ldv, quake_dtype dtype,
                              quake_mode mode, float t, int causal, void* stream);
+
+/*
+ * quake_attention_window — attention over a key/value cache with a sliding
+ * window and sink tokens: o_i = sum_j p_ij v_j / sum_j p_ij over the keys j that
+ * query i sees,
+ *   j <= pos_i  and  (j > pos_i - window  or  j < sinks),
+ *   pos_i = kv_len - q_len + i   (the queries are the last tokens of the keys),
+ * p_ij = the exponential of `mode` of t q_i.k_j. For a prompt sq = skv; for one
+ * new token per sequence sq = 1 and the cache holds its key and value already;
+ * anything between continues a sequence. A query that sees no key (pos_i < 0)
+ * gets zeros. `heads` query heads share kv_heads key heads (a divisor of heads):
+ * query head n reads key head n / (heads / kv_heads).
+ * The exponentials are taken against a whole number M of base-2 units, not the
+ * row max of Algorithm 2: QuAKE(y - M) = 2^-M QuAKE(y) exactly for a whole M
+ * (Eq. 3: M moves the exponent field only), so partial results join exactly and
+ * the keys are read once. They are the values Algorithm 2's would have up to one
+ * common factor per row and that factor's place in the period of the
+ * approximation's error; each is within the mode's error of e^(t s).
+ * Probabilities are rounded to the 16-bit format before the second product, sums
+ * and products are binary32, the quotient is rounded once.
+ *   q, o : device, batch x sq tokens x heads x dim, dtype; k, v : device,
+ *          batch x skv tokens x kv_heads x dim, dtype. dim (64 or 128) is
+ *          contiguous; the other strides, in elements, are in `strides` (host
+ *          pointer): of the batch, the token and the head. Each is >= 0 and a
+ *          multiple of 8 (of a size of 1: anything), the key and value tokens' at
+ *          most 2^24; all pointers 16-byte aligned. o overlaps nothing.
+ *   q_lens, kv_lens : device int32, one per sequence, or NULL (sq, skv): tokens
+ *          each sequence has in the padded buffers, clamped to 0 .. sq and
+ *          0 .. skv. Queries from q_len on are not read and their o is left as it
+ *          was; keys from kv_len on, and keys that no query of a tile sees, are
+ *          not read.
+ *   window : 1 .. 2^31 - 1 (skv or more: causal attention); sinks : 0 .. 2^31 - 1.
+ *   workspace : device, 16-byte aligned, of the size that
+ *          quake_attention_window_workspace_size gives for these sizes (0: none
+ *          needed), any content; a call's keys are then split over more
+ *          workgroups. NULL: never split. Calls that may run at the same time need
+ *          workspaces of their own.
+ *   batch <= 2^24, sq <= 2^24, skv <= 2^30, heads <= 2^16, and at most 2^24 tiles
+ *   of 32 rows (a row: one query of one head); dtype QUAKE_BF16 or QUAKE_F16 (else
+ *   QUAKE_EDTYPE); t as in quake_attention. batch == 0 or sq == 0 launches nothing.
+ * A visible key or value that is not finite may spoil the outputs of other queries
+ * of its sequence and key head, those that do not see it among them.
+ */
+typedef struct {
+  int64_t q[3], k[3], v[3], o[3]; /* batch, token, head */
+} quake_window_strides;
+
+quake_status quake_attention_window_workspace_size(int64_t batch, int64_t sq, int64_t skv,
+                                                   int64_t heads, int64_t kv_heads, int64_t dim,
+                                                   int64_t window, int64_t sinks, int64_t* bytes);
+quake_status quake_attention_window(const void* q, const void* k, const void* v, void* o,
+                                    const int32_t* q_lens, const int32_t* kv_lens, int64_t batch,
+                                    int64_t sq, int64_t skv, int64_t heads, int64_t kv_heads,
+                                    int64_t dim, const quake_window_strides* strides,
+                                    int64_t window, int64_t sinks, quake_dtype dtype,
+                                    quake_mode mode, float t, void* workspace,
+                                    int64_t workspace_bytes, void* stream);
+
+/*
+ * quake_sample — the next token of every row of logits from one given random
+ * number per row, after temperature, top-k, top-p and min-p. With m the row max,
+ * w_i = the exponential of `mode` of (x_i - m) / temperature (l = fmaf(x_i - m, c0,
+ * 127 * 2^23), c0 = fl32(2^23 / (temperature ln2)); 1 where x_i = m) and
+ * W_i = floor(w_i 2^40), a 64-bit integer, words are ranked by w descending, equal
+ * ones by index ascending, and a word is kept that passes all of
+ *   top-k  its rank is below k (then the ranking and Z are those of the words left),
+ *   top-p  the words ranked before it have W summing below floor(p Z), Z the sum
+ *          of all W (the first word is always kept),
+ *   min-p  W_i >= floor(min_p 2^40), and W_i > 0.
+ * token[r] = the first kept word in index order at which the running sum of kept W
+ * exceeds floor(u Z'), Z' their whole sum; prob[r] = W / Z' of that word. p, min_p
+ * and u are cut to 24 binary digits. All sums are exact, so the token is a function
+ * of the inputs alone: the same bits of w give the same token whatever the
+ * workspace (QUAKE_EXACT's w is the hardware exponential's).
+ *   x     : device, rows x cols, row r at x + r*ldx (elements), any alignment;
+ *           1 <= cols <= 2^22, ldx >= cols. Words of -inf or NaN are never drawn.
+ *   u     : device float, one per row, in [0, 1) (clamped; NaN: 0).
+ *   token : device int32, one per row; -1 (prob 0) where no word is above -inf.
+ *   prob  : device float, one per row, or NULL.
+ *   temperature, top_k, top_p, min_p : device, one per row (top_k int32, the others
+ *           float), or NULL: 1, and no filter. temperature <= 0 or NaN: the largest
+ *           logit, the first of equal ones. top_k <= 0 or >= cols, top_p >= 1 or
+ *           NaN, min_p <= 0 or NaN: no such filter for the row; top_p <= 0 keeps one
+ *           word; min_p > 1 counts as 1.
+ *   workspace : device, 16-byte aligned, of the size quake_sample_workspace_size
+ *           gives (0: none needed), any content: a row is then read by several
+ *           workgroups. NULL: one workgroup per row. Calls that may run at the same
+ *           time need workspaces of their own.
+ * rows == 0 launches nothing.
+ */
+quake_status quake_sample_workspace_size(int64_t rows, int64_t cols, int64_t* bytes);
+quake_status quake_sample(const void* x, const float* u, int32_t* token, float* prob, int64_t rows,
+                          int64_t cols, int64_t ldx, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p,
+                          quake_dtype dtype, quake_mode mode, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+
+/*
+ * quake_distill — distillation from a teacher's top logits: with p = softmax(t y)
+ * over the row's entries and q = softmax(t x) over the vocabulary, both with the
+ * exponential of `mode`,
+ *   loss[r] = sum_k p_k (log p_k - log q_{idx_k}),
+ *   grad[r, v] = weight[r] t (q_v - sum_{k : idx_k = v} p_k)   (grad != NULL).
+ * The logarithms are t times the logit less the logarithm of its softmax's sum
+ * (natural); the gradient is the formula's, with the q and p of `mode`. Multiply
+ * weight by 1 / t^2 for the usual temperature scaling. The exponentials are taken
+ * against M = ceil(t max / ln2) (see quake_attention_window).
+ *   x    : device, rows x cols logits of `dtype`, row r at x + r*ldx.
+ *   idx  : device int32, y : device, `ydtype`; rows x topk, rows ldi and ldy apart.
+ *          Entries whose idx lies outside 0 .. cols-1 are left out (padding);
+ *          an index that comes twice counts twice. A row with no entry has loss 0
+ *          and gradient 0. An entry with y = -inf has p = 0.
+ *   weight : device float, one per row, or NULL (1). 0: the row's gradient is 0.
+ *   loss : device float, one per row, not weighted. +inf where an entry with p > 0
+ *          meets a logit of -inf.
+ *   stats: device float, rows x 2: M and S = sum_v QuAKEx(t x_v / ln2 - M), what
+ *          quake_distill_grad needs; or NULL.
+ *   grad : device, `dtype`, row r at grad + r*ldg; may be x itself (ldg == ldx);
+ *          otherwise it overlaps nothing. NULL: no gradient (ldg unused).
+ *   cols <= 2^30, topk <= 1024, ldx, ldg >= cols, ldi, ldy >= topk; t as in
+ *   quake_softmax. Logits of +inf or NaN: unspecified. |t x| below 1e6.
+ *   workspace : device, 16-byte aligned, of the size quake_distill_workspace_size
+ *          gives (0: none needed), any content: few rows are then cut into chunks.
+ *          NULL: one workgroup per row. Calls that may run at the same time need
+ *          workspaces of their own.
+ * Rows are read as the aligned 16-byte vectors that cover them (up to 15 bytes
+ * around a row, never outside such a vector) and written inside only. Sums are
+ * binary32 within a vector, then binary64 in a fixed order: the same bits every time.
+ * quake_distill_grad is the gradient alone, from the same x, idx, y, mode, t and the
+ * stats that quake_distill gave, where its weight is known only later.
+ */
+quake_status quake_distill_workspace_size(int64_t rows, int64_t cols, int64_t* bytes);
+quake_status quake_distill(const void* x, const int32_t* idx, const void* y, const float* weight,
+                           float* loss, float* stats, void* grad, int64_t rows, int64_t cols,
+                           int64_t topk, int64_t ldx, int64_t ldi, int64_t ldy, int64_t ldg,
+                           quake_dtype dtype, quake_dtype ydtype, quake_mode mode, float t,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+quake_status quake_distill_grad(const void* x, const int32_t* idx, const void* y,
+                                const float* stats, const float* weight, void* grad, int64_t rows,
+                                int64_t cols, int64_t topk, int64_t ldx, int64_t ldi, int64_t ldy,
+                                int64_t ldg, quake_dtype dtype, quake_dtype ydtype,
+                                quake_mode mode, float t, void* stream);
 
 /*
  * quake_stream_copy — a measurement aid, not part of the method: copies

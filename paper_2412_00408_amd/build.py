@@ -24,7 +24,7 @@ C_CLIENT = os.path.join(ROOT, "tests", "c", "abi_smoke")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 SOURCES = ["elementwise.hip", "softmax.hip", "native16.hip", "gemm.hip", "attention.hip",
-           "ceiling.hip", "abi.cpp"]
+           "window.hip", "sample.hip", "distill.hip", "ceiling.hip", "abi.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [
@@ -34,9 +34,10 @@ FLAGS = [
 ]
 
 
-# Matrix-core accumulators in ordinary VGPRs: the attention kernel feeds them
+# Matrix-core accumulators in ordinary VGPRs: the attention kernels feed them
 # straight to VALU work, which cannot read the accumulation registers.
-EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:

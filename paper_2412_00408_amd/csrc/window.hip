@@ -1,0 +1,530 @@
+// window.hip — quake_attention_window: attention over a key/value cache with a
+// sliding window and sink tokens, o_i = sum_j p_ij v_j / sum_j p_ij over the keys
+// query i sees (j <= pos_i and (j > pos_i - window or j < sinks)).
+//
+// The exponentials are QuAKE's (arXiv:2412.00408), taken against a whole number M
+// of base-2 units instead of the row max itself: Q(y - M) = 2^-M Q(y) exactly for
+// the bit constructions too, as M only moves the exponent field (l of Eq. 5 moves
+// by M 2^23, its mantissa bits stay). So here, unlike in Algorithm 2 with its
+// real-valued max, a running M can be raised later by an exact power of two: the
+// keys are read once, and partial results of different keys join exactly,
+// whatever their number and order. c1 = (127 - M) 2^23 is exact in binary32, so
+// l = fma(s, c0, c1) has one rounding. M follows the running max lazily, only
+// when it falls more than kLazy below (probabilities then reach 2^kLazy, which
+// binary32 sums and both 16-bit formats hold with the same relative rounding).
+//
+// Rows. The queries of all heads that share a key head are one list of rows,
+// row r = query r / group, head r mod group of the group, so a single token's
+// group fills one tile and a tile of a prompt covers few positions, whose windows
+// nearly coincide. Keys. A tile's keys are the list "sinks below the window, then
+// the window" (Span), cut into blocks of 32 from its first key on, not at
+// multiples of 32; keys that no row of the tile sees are never read.
+//
+// Products (matrix cores, v_mfma_f32_32x32x16): S^T = K Q^T with K staged in LDS,
+// lane l then holding row l mod 32 and keys 8 g + 4 (l / 32) + i of the block,
+// i, g < 4; O^T = V^T P with the same lane's exponentials as the B operand as they
+// lie: the 16 keys of a step are numbered 8 (e / 4) + 4 (l / 32) + e mod 4, e < 8,
+// on both sides, so nothing is exchanged between lanes. The A operand, V^T, comes
+// from V's rows in LDS by ds_read_b64_tr_b16 (16 lanes read 4 keys x 16 dims and
+// each receives its dim's 4 keys), so V needs no transposed copy.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "quake_device.hpp"
+#include "quake_host.hpp"
+
+namespace qk {
+
+typedef __bf16 wbf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 wf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLazy = 8.0f;      // how far the running max may rise above M
+constexpr float kNoMax = -1e30f;   // M of a row that has seen no key
+constexpr int kWinWaves = 4;
+
+struct WindowArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* o;
+  const int32_t *q_lens, *kv_lens;   // or null: sq, skv
+  float* ws;                         // partial results, nsplit > 1
+  int64_t qb, qs, qh, kb, ks, kh, vb, vs, vh, ob, os, oh;   // strides in elements
+  int32_t sq, skv, group, kv_heads, tiles, nsplit;
+  uint32_t window, sinks;
+  float c0;                          // 2^23 t / ln2 (EXACT: t / ln2)
+};
+
+template <int DT>
+__device__ __forceinline__ f32x16 wmma(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (DT == BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(wbf16x8_t, a),
+                                                   __builtin_bit_cast(wbf16x8_t, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(wf16x8_t, a),
+                                                  __builtin_bit_cast(wf16x8_t, b), c, 0, 0, 0);
+}
+template <int DT>
+__device__ __forceinline__ uint32_t wpack(float a, float b) {
+  return DT == BF16 ? pack_bf16(a, b) : pack_f16(a, b);
+}
+__device__ __forceinline__ float other_half(float v) {   // the value of lane l xor 32
+  const auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+  return as_f((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// The keys of a tile of rows at positions first .. last: number n of the list is
+// key n below `sinks` (of them those below the window), else key n + shift.
+struct Span {
+  int32_t sinks, shift, total;
+  __device__ __forceinline__ Span(int32_t first, int32_t last, const WindowArgs& g) {
+    int32_t low = 0;
+    if (first >= 0 && (uint32_t)first >= g.window) low = first - (int32_t)g.window + 1;
+    sinks = 0;
+    if (g.sinks < (uint32_t)low)
+      sinks = (int32_t)g.sinks;
+    else
+      low = 0;
+    shift = low - sinks;
+    total = last < 0 ? 0 : last + 1 - shift;
+  }
+  __device__ __forceinline__ int32_t key(int32_t n) const { return n < sinks ? n : n + shift; }
+};
+
+// Blocks of 32 keys in LDS, rows of D 16-bit elements in 16-byte chunks; chunk c
+// of row r sits at chunk c ^ swizzle(r). K's operand reads take one chunk of 32
+// consecutive rows, V's transposed reads 64 bytes of 8 consecutive rows: with
+// these swizzles neither meets a bank twice beyond what its width costs.
+template <int D>
+__device__ __forceinline__ int kswizzle(int r) {
+  return D == 128 ? (r & 15) : ((r & 7) ^ ((r >> 3) & 1));
+}
+template <int D>
+__device__ __forceinline__ int vswizzle(int r) {
+  return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
+}
+
+// Loads keys n0 .. n0 + 31 of the list into an LDS block (1024 bytes a load:
+// 64 lanes x 16). Whole blocks of the window go from a uniform base; blocks that
+// hold sinks or end behind the list from each lane's own row, the list's last key
+// standing for those behind it (their probabilities are 0).
+template <int D, bool IS_V>
+__device__ __forceinline__ void stage_block(uint32_t lds, const uint16_t* base, int64_t stride,
+                                            const Span& sp, int32_t n0, int lane) {
+  constexpr int CH = D / 8, RPL = 64 / CH, N = 32 / RPL;   // chunks a row, rows a load, loads
+  const int r = lane / CH, pc = lane % CH;
+  if (n0 >= sp.sinks && n0 + 32 <= sp.total) {
+    const char* b = scalar_base(base + (int64_t)(n0 + sp.shift) * stride);
+    const uint32_t row = (uint32_t)r * (uint32_t)stride * 2u;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int sw = IS_V ? vswizzle<D>(RPL * j + r) : kswizzle<D>(RPL * j + r);
+      lds_load16(lds + 1024 * j, row + 16u * (uint32_t)(pc ^ sw), b + (int64_t)2 * RPL * j * stride);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int sw = IS_V ? vswizzle<D>(RPL * j + r) : kswizzle<D>(RPL * j + r);
+      const int32_t key = sp.key(min(n0 + RPL * j + r, sp.total - 1));
+      lds_load16(lds + 1024 * j, base + (int64_t)key * stride + 8 * (pc ^ sw));
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ u32x4 read_k(const char* blk, int fr, int h, int ks) {
+  return *reinterpret_cast<const u32x4*>(blk + fr * (2 * D) + 16 * ((2 * ks + h) ^ kswizzle<D>(fr)));
+}
+// dims 32 db + lane mod 32, keys 16 ks + 8 u + 4 h + 0 .. 3, u = 0, 1
+template <int D>
+__device__ __forceinline__ u32x4 read_v(const char* blk, int lane, int ks, int db) {
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  u32x2 p[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = 16 * ks + 8 * u + 4 * (lane >> 5) + ((lane >> 2) & 3);
+    const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    const char* a = blk + row * (2 * D) + 16 * (c ^ vswizzle<D>(row)) + 8 * (lane & 1);
+    p[u] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)a));
+  }
+  return u32x4{p[0][0], p[0][1], p[1][0], p[1][1]};
+}
+
+// 2^(from - to), from <= to whole numbers, as an exponent
+__device__ __forceinline__ int32_t down_shift(float from, float to) {
+  return (int32_t)fmaxf(from - to, -1000.0f);
+}
+
+// What a row has accumulated: D / 32 blocks of O^T, this lane's part of the sum.
+template <int D>
+struct RowAcc {
+  f32x16 o[D / 32];
+  float sum, m;
+};
+
+// The scores of one block to the probabilities (16-bit pairs of keys as they
+// lie), raising M and rescaling what is accumulated where the max asks for it.
+template <int DT, int MODE, int D>
+__device__ __forceinline__ void softmax_block(const f32x16& s, float c0, RowAcc<D>& acc,
+                                              u32x4 (&p)[2]) {
+  constexpr float kScale = MODE == EXACT ? 1.0f : 0x1p-23f;
+  float top = s[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+  top = fmaxf(top, other_half(top)) * (c0 * kScale);
+  if (__any(top > acc.m + kLazy)) {
+    const float m = top > acc.m + kLazy ? __builtin_ceilf(top) : acc.m;
+    const int32_t e = down_shift(acc.m, m);
+    acc.m = m;
+    acc.sum = __builtin_amdgcn_ldexpf(acc.sum, e);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc.o[d][r] = __builtin_amdgcn_ldexpf(acc.o[d][r], e);
+  }
+  const float c1 = MODE == EXACT ? -acc.m : (127.0f - acc.m) * 0x1p23f;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    float e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e[i] = qexp_row<MODE, true>(s[4 * g + i], c0, c1);
+      acc.sum += e[i];
+    }
+    p[g >> 1][2 * (g & 1)] = wpack<DT>(e[0], e[1]);
+    p[g >> 1][2 * (g & 1) + 1] = wpack<DT>(e[2], e[3]);
+  }
+}
+
+// -inf for the keys of block n0 that the row at `pos` does not see
+__device__ __forceinline__ void mask_block(f32x16& s, const Span& sp, int32_t n0, int32_t pos,
+                                           int h, const WindowArgs& g) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int32_t key = sp.key(n0 + 8 * (r >> 2) + 4 * h + (r & 3));
+    const uint32_t limit = (uint32_t)key < g.sinks ? 0x80000000u : g.window;
+    s[r] = (uint32_t)(pos - key) < limit ? s[r] : -INFINITY;
+  }
+}
+
+__device__ __forceinline__ int32_t seq_len(const int32_t* lens, int b, int32_t most) {
+  return lens == nullptr ? most : min(max(lens[b], 0), most);
+}
+
+// A tile of 32 rows in one workgroup; the waves take every fourth block of its
+// keys and join at the end. What bounds it is reading the keys (single tokens),
+// so each wave keeps the next block's K and V in flight.
+template <int DT, int MODE, int D>
+__global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g) {
+  constexpr int kBlk = 64 * D;                      // bytes of a block of 32 rows
+  constexpr int kWave = 4 * kBlk;                   // K and V, two buffers
+  __shared__ __attribute__((aligned(16))) char s_buf[kWinWaves * kWave];
+  __shared__ float s_m[kWinWaves][32], s_sum[kWinWaves][32];
+
+  const int lane = threadIdx.x & 63, fr = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.x % (uint32_t)g.nsplit;
+  const uint32_t item = blockIdx.x / (uint32_t)g.nsplit;
+  const int tile = item % (uint32_t)g.tiles;
+  const int hk = (item / (uint32_t)g.tiles) % (uint32_t)g.kv_heads;
+  const int b = item / (uint32_t)g.tiles / (uint32_t)g.kv_heads;
+  const int32_t qlen = seq_len(g.q_lens, b, g.sq), kvlen = seq_len(g.kv_lens, b, g.skv);
+  const int32_t rows = qlen * g.group, r0 = 32 * tile;
+  if (r0 >= rows) return;
+  const int32_t row = min(r0 + fr, rows - 1);
+  const int32_t first = kvlen - qlen + r0 / g.group;
+  const int32_t last = kvlen - qlen + min(r0 + 31, rows - 1) / g.group;
+  const int32_t query = row / g.group, head = hk * g.group + row % g.group;
+  const int32_t pos = kvlen - qlen + query;
+  const Span sp(first, last, g);
+  const int32_t blocks = (sp.total + 31) >> 5;
+  const int32_t n_lo = (int32_t)((int64_t)blocks * split / g.nsplit);
+  const int32_t n_hi = (int32_t)((int64_t)blocks * (split + 1) / g.nsplit);
+
+  u32x4 qf[D / 16];
+  {
+    const uint16_t* qr = g.q + b * g.qb + query * g.qs + head * g.qh + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(qr + 16 * ks);
+  }
+  const uint16_t* K = g.k + b * g.kb + hk * g.kh;
+  const uint16_t* V = g.v + b * g.vb + hk * g.vh;
+  char* buf = s_buf + wave * kWave;
+  const uint32_t lds =
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf + wave * kWave;
+  auto load = [&](int32_t n, int slot) {
+    stage_block<D, false>(lds + 2 * kBlk * slot, K, g.ks, sp, 32 * n, lane);
+    stage_block<D, true>(lds + 2 * kBlk * slot + kBlk, V, g.vs, sp, 32 * n, lane);
+  };
+
+  RowAcc<D> acc;
+  acc.sum = 0.0f;
+  acc.m = kNoMax;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) acc.o[d] = f32x16{};
+  if (n_lo + wave < n_hi) load(n_lo + wave, 0);
+  int slot = 0;
+  for (int32_t n = n_lo + wave; n < n_hi; n += kWinWaves, slot ^= 1) {
+    if (n + kWinWaves < n_hi) {
+      load(n + kWinWaves, slot ^ 1);
+      wait_loads<D / 8>();   // of the next block: D / 16 loads each for K and V
+    } else {
+      wait_loads<0>();
+    }
+    const char* kblk = buf + 2 * kBlk * slot;
+    f32x16 s = {};
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) s = wmma<DT>(read_k<D>(kblk, fr, h, ks), qf[ks], s);
+    // every key of the block seen by every row of the tile: no mask
+    const int32_t ka = sp.key(32 * n), kz = sp.key(32 * n + 31);
+    const bool all = kz <= first && (kz - ka == 31) &&
+                     ((uint32_t)kz < g.sinks || (uint32_t)(last - ka) < g.window);
+    if (!all) mask_block(s, sp, 32 * n, pos, h, g);
+    u32x4 p[2];
+    softmax_block<DT, MODE, D>(s, g.c0, acc, p);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+        acc.o[d] = wmma<DT>(read_v<D>(kblk + kBlk, lane, ks, d), p[ks], acc.o[d]);
+    wait_lds();   // this buffer's reads, before it is loaded again
+  }
+
+  // join the waves: their M, then sums and O^T brought to the largest M
+  acc.sum += other_half(acc.sum);
+  __syncthreads();   // every wave is done with its buffers
+  if (lane < 32) {
+    s_m[wave][fr] = acc.m;
+    s_sum[wave][fr] = acc.sum;
+  }
+  float* part = reinterpret_cast<float*>(s_buf + wave * kWave);   // [D][32] floats
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      part[(32 * d + 8 * (r >> 2) + 4 * h + (r & 3)) * 32 + fr] = acc.o[d][r];
+  __syncthreads();
+  float m = s_m[0][fr];
+#pragma unroll
+  for (int w = 1; w < kWinWaves; ++w) m = fmaxf(m, s_m[w][fr]);
+  float sum = 0.0f;
+  int32_t e[kWinWaves];
+#pragma unroll
+  for (int w = 0; w < kWinWaves; ++w) {
+    e[w] = down_shift(s_m[w][fr], m);
+    sum += __builtin_amdgcn_ldexpf(s_sum[w][fr], e[w]);
+  }
+  // this wave's dims: D / 4, each half of its lanes D / 8 of them
+  constexpr int N = D / 8;
+  const int d0 = wave * (D / 4) + h * N;
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWinWaves; ++w)
+      v[i] += __builtin_amdgcn_ldexpf(
+          reinterpret_cast<const float*>(s_buf + w * kWave)[(d0 + i) * 32 + fr], e[w]);
+  }
+  if (g.nsplit > 1) {
+    float* w = g.ws + (int64_t)blockIdx.x * (64 + 32 * D);
+    if (wave == 0 && h == 0) {
+      w[fr] = m;
+      w[32 + fr] = sum;
+    }
+    float4* wo = reinterpret_cast<float4*>(w + 64 + fr * D + d0);
+#pragma unroll
+    for (int i = 0; i < N; i += 4) wo[i / 4] = float4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    return;
+  }
+  if (r0 + fr >= rows) return;
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  uint16_t* orow = g.o + b * g.ob + query * g.os + head * g.oh + d0;
+#pragma unroll
+  for (int i = 0; i < N; i += 8) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = wpack<DT>(v[i + 2 * j] * inv, v[i + 2 * j + 1] * inv);
+    *reinterpret_cast<u32x4*>(orow + i) = w;
+  }
+}
+
+// Joins the splits of a tile: thread t takes D / 8 dims of row t / 8.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void window_join_kernel(WindowArgs g) {
+  const int tile = blockIdx.x % (uint32_t)g.tiles;
+  const int hk = (blockIdx.x / (uint32_t)g.tiles) % (uint32_t)g.kv_heads;
+  const int b = blockIdx.x / (uint32_t)g.tiles / (uint32_t)g.kv_heads;
+  const int32_t rows = seq_len(g.q_lens, b, g.sq) * g.group;
+  const int fr = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * (D / 8);
+  const int32_t row = 32 * tile + fr;
+  if (row >= rows) return;
+  const int64_t slot = 64 + 32 * D;
+  const float* w = g.ws + (int64_t)blockIdx.x * g.nsplit * slot;
+  float m = kNoMax;
+  for (int s = 0; s < g.nsplit; ++s) m = fmaxf(m, w[s * slot + fr]);
+  float sum = 0.0f, v[D / 8] = {};
+  for (int s = 0; s < g.nsplit; ++s) {
+    const int32_t e = down_shift(w[s * slot + fr], m);
+    sum += __builtin_amdgcn_ldexpf(w[s * slot + 32 + fr], e);
+#pragma unroll
+    for (int i = 0; i < D / 8; i += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(w + s * slot + 64 + fr * D + d0 + i);
+      v[i] += __builtin_amdgcn_ldexpf(x.x, e);
+      v[i + 1] += __builtin_amdgcn_ldexpf(x.y, e);
+      v[i + 2] += __builtin_amdgcn_ldexpf(x.z, e);
+      v[i + 3] += __builtin_amdgcn_ldexpf(x.w, e);
+    }
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  uint16_t* orow = g.o + b * g.ob + (row / g.group) * g.os +
+                   (hk * g.group + row % g.group) * g.oh + d0;
+#pragma unroll
+  for (int i = 0; i < D / 8; i += 8) {
+    u32x4 x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = wpack<DT>(v[i + 2 * j] * inv, v[i + 2 * j + 1] * inv);
+    *reinterpret_cast<u32x4*>(orow + i) = x;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+struct WindowPlan {
+  int64_t tiles;    // row tiles of a key head
+  int64_t nsplit;   // workgroups that share a tile's keys
+};
+
+// Splits: few tiles leave compute units idle while each walks a long window, so a
+// tile's keys go to as many workgroups as bring the launch to kWinTarget, with at
+// least 8 blocks of 32 keys (two a wave) for each.
+constexpr int64_t kWinTarget = 512;
+
+static WindowPlan window_plan(int64_t batch, int64_t sq, int64_t skv, int64_t group,
+                              int64_t kv_heads, int64_t window, int64_t sinks) {
+  WindowPlan p;
+  p.tiles = (sq * group + 31) / 32;
+  const int64_t items = batch * kv_heads * p.tiles;
+  const int64_t queries = (31 + group) / group;   // most positions a tile covers, less one
+  const int64_t keys = std::min(skv, std::min(window, skv) + std::min(sinks, skv) + queries);
+  const int64_t most = (keys + 255) / 256;
+  p.nsplit = items == 0 ? 1 : std::max<int64_t>(1, std::min(most, kWinTarget / items));
+  return p;
+}
+
+static int64_t window_ws_bytes(const WindowPlan& p, int64_t batch, int64_t kv_heads, int64_t dim) {
+  if (p.nsplit == 1) return 0;
+  return batch * kv_heads * p.tiles * p.nsplit * (64 + 32 * dim) * 4;
+}
+
+static bool window_shape_ok(int64_t batch, int64_t sq, int64_t skv, int64_t heads,
+                            int64_t kv_heads, int64_t dim, int64_t window, int64_t sinks) {
+  if (batch < 0 || sq < 0 || skv < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0)
+    return false;
+  if ((dim != 64 && dim != 128) || window < 1 || sinks < 0) return false;
+  if (window > INT32_MAX || sinks > INT32_MAX || skv > (1 << 30) || sq > (1 << 24)) return false;
+  if (heads > (1 << 16) || batch > (1 << 24)) return false;
+  if (sq * (heads / kv_heads) > (1 << 30)) return false;
+  return batch * kv_heads * ((sq * (heads / kv_heads) + 31) / 32) <= (1 << 24);
+}
+
+template <int DT, int D>
+static void launch_window(int mode, dim3 grid, hipStream_t s, const WindowArgs& g) {
+  const dim3 block(64 * kWinWaves);
+  switch (mode) {
+    case QUAKE_EXACT: hipLaunchKernelGGL((window_few_kernel<DT, EXACT, D>), grid, block, 0, s, g); break;
+    case QUAKE_1: hipLaunchKernelGGL((window_few_kernel<DT, Q1, D>), grid, block, 0, s, g); break;
+    case QUAKE_2: hipLaunchKernelGGL((window_few_kernel<DT, Q2, D>), grid, block, 0, s, g); break;
+    default: hipLaunchKernelGGL((window_few_kernel<DT, Q2M, D>), grid, block, 0, s, g); break;
+  }
+  if (g.nsplit > 1)
+    hipLaunchKernelGGL((window_join_kernel<DT, D>), dim3(grid.x / g.nsplit), dim3(256), 0, s, g);
+}
+
+}  // namespace qk
+
+using namespace qk;
+
+extern "C" quake_status quake_attention_window_workspace_size(int64_t batch, int64_t sq,
+                                                              int64_t skv, int64_t heads,
+                                                              int64_t kv_heads, int64_t dim,
+                                                              int64_t window, int64_t sinks,
+                                                              int64_t* bytes) {
+  if (bytes == nullptr) return QUAKE_EINVAL;
+  if (!window_shape_ok(batch, sq, skv, heads, kv_heads, dim, window, sinks)) return QUAKE_EINVAL;
+  const WindowPlan p = window_plan(batch, sq, skv, heads / kv_heads, kv_heads, window, sinks);
+  *bytes = window_ws_bytes(p, batch, kv_heads, dim);
+  return QUAKE_OK;
+}
+
+extern "C" quake_status quake_attention_window(
+    const void* q, const void* k, const void* v, void* o, const int32_t* q_lens,
+    const int32_t* kv_lens, int64_t batch, int64_t sq, int64_t skv, int64_t heads,
+    int64_t kv_heads, int64_t dim, const quake_window_strides* strides, int64_t window,
+    int64_t sinks, quake_dtype dtype, quake_mode mode, float t, void* workspace,
+    int64_t workspace_bytes, void* stream) {
+  if (dtype != QUAKE_BF16 && dtype != QUAKE_F16) return QUAKE_EDTYPE;
+  if (!valid_mode(mode)) return QUAKE_EMODE;
+  if (!window_shape_ok(batch, sq, skv, heads, kv_heads, dim, window, sinks)) return QUAKE_EINVAL;
+  if (!std::isfinite(t) || !(t > 0.0f)) return QUAKE_EINVAL;
+  const float c0 = softmax_c0(t, mode);
+  if (!std::isfinite(c0) || c0 == 0.0f) return QUAKE_EINVAL;
+  if (workspace_bytes < 0 || (workspace != nullptr && !aligned16(workspace))) return QUAKE_EINVAL;
+  if (batch == 0 || sq == 0) return QUAKE_OK;
+  if (strides == nullptr || q == nullptr || o == nullptr) return QUAKE_EINVAL;
+  if (skv > 0 && (k == nullptr || v == nullptr)) return QUAKE_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) ||
+      ((uintptr_t)q_lens & 3u) != 0 || ((uintptr_t)kv_lens & 3u) != 0)
+    return QUAKE_EINVAL;
+  const quake_window_strides& st = *strides;
+  const int64_t n[4] = {batch, sq, skv, 1};
+  for (int i = 0; i < 3; ++i) {
+    const int64_t count = i == 0 ? batch : i == 1 ? 0 : heads;   // tokens: per operand below
+    for (const int64_t* s : {st.q, st.k, st.v, st.o}) {
+      const bool kv = s == st.k || s == st.v;
+      const int64_t c = i == 1 ? (kv ? n[2] : n[1]) : (i == 2 && kv) ? kv_heads : count;
+      if (c <= 1) continue;   // never multiplied by anything but 0
+      if (s[i] < 0 || s[i] % 8 != 0 || s[i] > INT64_MAX / 8 / c) return QUAKE_EINVAL;
+      if (i == 1 && kv && s[i] > (1 << 24)) return QUAKE_EINVAL;   // 32-row offsets in 32 bits
+    }
+  }
+  const WindowPlan p = window_plan(batch, sq, skv, heads / kv_heads, kv_heads, window, sinks);
+  const int64_t need = window_ws_bytes(p, batch, kv_heads, dim);
+  const bool split = workspace != nullptr && need > 0;
+  if (split && workspace_bytes < need) return QUAKE_EINVAL;
+  WindowArgs g{};
+  g.q = static_cast<const uint16_t*>(q);
+  g.k = static_cast<const uint16_t*>(k);
+  g.v = static_cast<const uint16_t*>(v);
+  g.o = static_cast<uint16_t*>(o);
+  g.q_lens = q_lens;
+  g.kv_lens = kv_lens;
+  g.ws = static_cast<float*>(workspace);
+  g.qb = st.q[0], g.qs = st.q[1], g.qh = st.q[2];
+  g.kb = st.k[0], g.ks = st.k[1], g.kh = st.k[2];
+  g.vb = st.v[0], g.vs = st.v[1], g.vh = st.v[2];
+  g.ob = st.o[0], g.os = st.o[1], g.oh = st.o[2];
+  g.sq = (int32_t)sq;
+  g.skv = (int32_t)skv;
+  g.group = (int32_t)(heads / kv_heads);
+  g.kv_heads = (int32_t)kv_heads;
+  g.tiles = (int32_t)p.tiles;
+  g.nsplit = split ? (int32_t)p.nsplit : 1;
+  g.window = (uint32_t)window;
+  g.sinks = (uint32_t)sinks;
+  g.c0 = c0;
+  const dim3 grid((uint32_t)(batch * kv_heads * p.tiles * g.nsplit));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == QUAKE_BF16) {
+    if (dim == 64) launch_window<BF16, 64>(mode, grid, s, g);
+    else launch_window<BF16, 128>(mode, grid, s, g);
+  } else {
+    if (dim == 64) launch_window<F16, 64>(mode, grid, s, g);
+    else launch_window<F16, 128>(mode, grid, s, g);
+  }
+  return launch_status();
+}

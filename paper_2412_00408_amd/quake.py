@@ -9,6 +9,7 @@ Build the library with ``python -m paper_2412_00408_amd.build``.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -49,7 +50,19 @@ def _load() -> ctypes.CDLL:
     L.quake_sigmoid.argtypes = [vp, vp, i64, ci, ci, ci, vp]
     L.quake_attention.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, cf, ci, vp]
     L.quake_stream_copy.argtypes = [vp, vp, i64, ci, vp]
-    for f in (L.quake_exp, L.quake_exp16, L.quake_linear_gelu, L.quake_softmax, L.quake_gelu,
+    fp, ip = vp, vp          # device pointers to float and int32
+    L.quake_attention_window.argtypes = [vp, vp, vp, vp, ip, ip, i64, i64, i64, i64, i64, i64,
+                                         ctypes.POINTER(ctypes.c_int64), i64, i64, ci, ci, cf, vp,
+                                         i64, vp]
+    L.quake_attention_window_workspace_size.argtypes = [i64] * 8 + [ctypes.POINTER(i64)]
+    L.quake_sample.argtypes = [vp, fp, ip, fp, i64, i64, i64, fp, ip, fp, fp, ci, ci, vp, i64, vp]
+    L.quake_sample_workspace_size.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    L.quake_distill.argtypes = [vp, ip, vp, fp, fp, fp, vp] + [i64] * 7 + [ci, ci, ci, cf, vp, i64, vp]
+    L.quake_distill_grad.argtypes = [vp, ip, vp, fp, fp, vp] + [i64] * 7 + [ci, ci, ci, cf, vp]
+    L.quake_distill_workspace_size.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    for f in (L.quake_attention_window, L.quake_attention_window_workspace_size, L.quake_sample,
+              L.quake_sample_workspace_size, L.quake_distill, L.quake_distill_grad,
+              L.quake_distill_workspace_size, L.quake_exp, L.quake_exp16, L.quake_linear_gelu, L.quake_softmax, L.quake_gelu,
               L.quake_softmax_ws, L.quake_softmax_workspace_size, L.quake_softmax_noalloc,
               L.quake_sigmoid, L.quake_attention, L.quake_stream_copy,
               L.quake_softmax_unfused, L.quake_gelu_unfused, L.quake_softmax_causal):
@@ -317,3 +330,257 @@ def quake_softmax_causal(x, y=None, period=None, shift=0, mode=QUAKE_2, t=1.0, w
         x.data_ptr(), y.data_ptr(), rows, cols, ldx, ldy, period, shift, int(bool(write_masked)),
         DTYPES[x.dtype], MODES[mode], t, _stream(x, stream)))
     return y
+
+
+# ---------------------------------------------------------------------------
+# Decoding and distillation: the operators that take several tensors. Each
+# launches on the device of its first tensor, whichever is current.
+# ---------------------------------------------------------------------------
+_STRIDES = ctypes.c_int64 * 12
+
+
+def _on(device):
+    """The device to launch on, as a context (none where it is current already)."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _operand(t, what, like=None, dtype=None, shape=None):
+    if not t.is_cuda:
+        raise ValueError("libquake takes device tensors")
+    if like is not None and t.device != like.device:
+        raise ValueError("%s must be on the device of the first tensor" % what)
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _per_row(t, what, x, n, dtype):
+    """Device pointer of a contiguous vector of n values, or None."""
+    if t is None:
+        return None
+    _operand(t, what, x, dtype, (n,))
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError("%s must be contiguous" % what)
+    return t.data_ptr()
+
+
+def _work(workspace, x):
+    if workspace is None:
+        return None, 0
+    _operand(workspace, "workspace", x)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _apart(out, what, *others):
+    o0, o1 = _span(out)
+    for t, name in others:
+        if t is not None:
+            a0, a1 = _span(t)
+            if o0 < a1 and a0 < o1:
+                raise ValueError("%s must not overlap %s" % (what, name))
+
+
+def _size(fn, *args):
+    c = ctypes.c_int64(0)
+    _raise(fn, getattr(lib, fn)(*args, ctypes.byref(c)))
+    return c.value
+
+
+def _new_workspace(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def attention_window_workspace(q, k, window, sinks=0):
+    """A workspace for quake_attention_window on tensors shaped like q and k, or
+    None when that shape needs none. Any content; one per stream."""
+    b, sq, heads, dim = q.shape
+    return _new_workspace(_size("quake_attention_window_workspace_size", b, sq, k.shape[1], heads,
+                                k.shape[2], dim, min(window, 2**31 - 1), sinks), q.device)
+
+
+def quake_attention_window(q, k, v, o=None, window=2**31 - 1, sinks=0, q_lens=None, kv_lens=None,
+                           mode=QUAKE_2, t=None, workspace=None, stream=None):
+    """Attention of the last q tokens of each sequence over its keys, query i
+    seeing keys j <= pos_i with j > pos_i - window or j < sinks: bfloat16 or
+    float16 q [batch, sq, heads, dim] and k, v [batch, skv, kv_heads, dim], dim 64
+    or 128 contiguous, other strides multiples of 8; heads a multiple of kv_heads.
+    q_lens, kv_lens: int32 [batch], the tokens each sequence has (default all);
+    rows of o past q_lens keep what they held (a new o: undefined). t defaults to
+    1/sqrt(dim). `workspace` (from attention_window_workspace) lets a call with few
+    rows split its keys over more workgroups."""
+    for a, what in ((q, "q"), (k, "k"), (v, "v")):
+        _operand(a, what, q)
+        if a.dtype not in DTYPES:
+            raise TypeError("libquake takes float32, float16 or bfloat16 tensors, got %s" % a.dtype)
+        if a.dim() != 4:
+            raise ValueError("%s needs [batch, tokens, heads, dim]" % what)
+        if a.dtype != q.dtype:
+            raise TypeError("q, k and v must have the same dtype")
+    batch, sq, heads, dim = q.shape
+    if k.shape != v.shape or k.shape[0] != batch or k.shape[3] != dim:
+        raise ValueError("k and v must be [batch, skv, kv_heads, dim] with q's batch and dim")
+    skv, kv_heads = k.shape[1], k.shape[2]
+    if kv_heads == 0 or heads % kv_heads:
+        raise ValueError("heads must be a multiple of kv_heads")
+    if o is None:
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    else:
+        _operand(o, "o", q, q.dtype, q.shape)
+        _apart(o, "o", (q, "q"), (k, "k"), (v, "v"), (q_lens, "q_lens"), (kv_lens, "kv_lens"))
+    for a, what in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
+        if a.stride(3) != 1:
+            raise ValueError("%s must have a contiguous last dimension" % what)
+    st = _STRIDES(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3])
+    ql = _per_row(q_lens, "q_lens", q, batch, torch.int32)
+    kl = _per_row(kv_lens, "kv_lens", q, batch, torch.int32)
+    ws, nbytes = _work(workspace, q)
+    t = 1.0 / dim ** 0.5 if t is None else t
+    with _on(q.device):
+        _raise("quake_attention_window", lib.quake_attention_window(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), ql, kl, batch, sq, skv, heads,
+            kv_heads, dim, st, min(window, 2**31 - 1), sinks, DTYPES[q.dtype], MODES[mode], t, ws,
+            nbytes, _stream(q, stream)))
+    return o
+
+
+def sample_workspace(x):
+    """A workspace for quake_sample on logits shaped like x [rows, cols], or None
+    when that shape needs none. Any content; one per stream."""
+    return _new_workspace(_size("quake_sample_workspace_size", x.shape[0], x.shape[1]), x.device)
+
+
+def _matrix(x, what):
+    _operand(x, what)
+    if x.dtype not in DTYPES:
+        raise TypeError("libquake takes float32, float16 or bfloat16 tensors, got %s" % x.dtype)
+    if x.dim() != 2:
+        raise ValueError("%s must be [rows, cols]" % what)
+    return _row_stride(x, what)
+
+
+def _row_stride(x, what):
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError("%s must have a contiguous last dimension" % what)
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def quake_sample(x, u, token=None, prob=None, temperature=None, top_k=None, top_p=None,
+                 min_p=None, mode=QUAKE_2, workspace=None, stream=None):
+    """The next token of every row of logits x [rows, cols] from the random numbers
+    u [rows] in [0, 1): returns (token, prob), int32 and float32 [rows], the words
+    drawn (-1: no word allowed) and their probabilities among the words kept.
+    temperature, top_p, min_p: float32 [rows], top_k: int32 [rows], or None (1, and
+    no filter); temperature 0 takes the largest logit. `workspace` (from
+    sample_workspace) lets several workgroups read a row."""
+    ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    if u is None:
+        raise ValueError("u must be float32 [rows]")
+    vecs = [_per_row(a, what, x, rows, dt) for a, what, dt in (
+        (u, "u", torch.float32), (temperature, "temperature", torch.float32),
+        (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
+        (min_p, "min_p", torch.float32))]
+    inputs = ((x, "x"), (u, "u"), (temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"),
+              (min_p, "min_p"))
+    if token is None:
+        token = torch.empty(rows, dtype=torch.int32, device=x.device)
+    else:
+        _per_row(token, "token", x, rows, torch.int32)
+        _apart(token, "token", *inputs)
+    if prob is None:
+        prob = torch.empty(rows, dtype=torch.float32, device=x.device)
+    else:
+        _per_row(prob, "prob", x, rows, torch.float32)
+        _apart(prob, "prob", (token, "token"), *inputs)
+    ws, nbytes = _work(workspace, x)
+    with _on(x.device):
+        _raise("quake_sample", lib.quake_sample(
+            x.data_ptr(), vecs[0], token.data_ptr(), prob.data_ptr(), rows, cols, ldx, *vecs[1:],
+            DTYPES[x.dtype], MODES[mode], ws, nbytes, _stream(x, stream)))
+    return token, prob
+
+
+def distill_workspace(x):
+    """A workspace for quake_distill on logits shaped like x [rows, cols], or None
+    when that shape needs none. Any content; one per stream."""
+    return _new_workspace(_size("quake_distill_workspace_size", x.shape[0], x.shape[1]), x.device)
+
+
+def _distill_args(x, idx, y, weight):
+    ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    topk = idx.shape[1] if idx.dim() == 2 else 0
+    _operand(idx, "idx", x, torch.int32, (rows, topk))
+    _operand(y, "y", x, None, (rows, topk))
+    if y.dtype not in DTYPES:
+        raise TypeError("libquake takes float32, float16 or bfloat16 tensors, got %s" % y.dtype)
+    return (rows, cols, topk, ldx, _row_stride(idx, "idx"), _row_stride(y, "y"),
+            _per_row(weight, "weight", x, rows, torch.float32))
+
+
+def _distill_grad_out(x, grad, *others):
+    """grad's row stride; x itself, or apart from every operand."""
+    _operand(grad, "grad", x, x.dtype, x.shape)
+    ldg = _row_stride(grad, "grad")
+    if grad.data_ptr() != x.data_ptr() or (x.shape[0] > 1 and grad.stride(0) != x.stride(0)):
+        _apart(grad, "grad", (x, "x"))
+    if grad.shape[0] > 1 and ldg < grad.shape[1]:
+        raise ValueError("grad's rows must not overlap")
+    _apart(grad, "grad", *others)
+    return ldg
+
+
+def quake_distill(x, idx, y, weight=None, grad=None, mode=QUAKE_2, t=1.0, workspace=None,
+                  stream=None):
+    """Distillation of x [rows, cols] from a teacher's top logits y [rows, topk] at
+    the words idx (int32; outside the vocabulary: no entry): returns (loss, stats,
+    grad): loss [rows], unweighted; stats [rows, 2] for quake_distill_grad; grad =
+    d(sum weight * loss)/dx, of x's dtype, where `grad` is True or a tensor to
+    write it to (x itself: in place), else None. `workspace` (from
+    distill_workspace) cuts few rows into chunks."""
+    rows, cols, topk, ldx, ldi, ldy, w = _distill_args(x, idx, y, weight)
+    ws, nbytes = _work(workspace, x)
+    loss = torch.empty(rows, dtype=torch.float32, device=x.device)
+    stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
+    ldg, gp = cols, None
+    if grad is True:
+        grad = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    elif grad is False:
+        grad = None
+    elif grad is not None:
+        ldg = _distill_grad_out(x, grad, (idx, "idx"), (y, "y"), (weight, "weight"))
+    if grad is not None:
+        gp = grad.data_ptr()
+    with _on(x.device):
+        _raise("quake_distill", lib.quake_distill(
+            x.data_ptr(), idx.data_ptr(), y.data_ptr(), w, loss.data_ptr(), stats.data_ptr(), gp,
+            rows, cols, topk, ldx, ldi, ldy, ldg, DTYPES[x.dtype], DTYPES[y.dtype], MODES[mode], t,
+            ws, nbytes, _stream(x, stream)))
+    return loss, stats, grad
+
+
+def quake_distill_grad(x, idx, y, stats, weight=None, grad=None, mode=QUAKE_2, t=1.0, stream=None):
+    """weight * d loss / dx of quake_distill(x, idx, y) from the stats it returned
+    (same mode and t), into `grad` (default a new tensor; x itself: in place)."""
+    rows, cols, topk, ldx, ldi, ldy, w = _distill_args(x, idx, y, weight)
+    _operand(stats, "stats", x, torch.float32, (rows, 2))
+    if not stats.is_contiguous():
+        raise ValueError("stats must be contiguous")
+    ldg = cols
+    if grad is None:
+        grad = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    else:
+        ldg = _distill_grad_out(x, grad, (idx, "idx"), (y, "y"), (weight, "weight"),
+                                (stats, "stats"))
+    with _on(x.device):
+        _raise("quake_distill_grad", lib.quake_distill_grad(
+            x.data_ptr(), idx.data_ptr(), y.data_ptr(), stats.data_ptr(), w, grad.data_ptr(), rows,
+            cols, topk, ldx, ldi, ldy, ldg, DTYPES[x.dtype], DTYPES[y.dtype], MODES[mode], t,
+            _stream(x, stream)))
+    return grad
