@@ -107,16 +107,17 @@ __device__ __forceinline__ int vswizzle(int r) {
   return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
 }
 
-// Loads keys n0 .. n0 + 31 of the list into an LDS block (1024 bytes a load:
-// 64 lanes x 16). Whole blocks of the window go from a uniform base; blocks that
-// hold sinks or end behind the list from each lane's own row, the list's last key
-// standing for those behind it (their probabilities are 0).
-template <int D, bool IS_V>
-__device__ __forceinline__ void stage_block(uint32_t lds, const uint16_t* base, int64_t stride,
-                                            const Span& sp, int32_t n0, int lane) {
-  constexpr int CH = D / 8, RPL = 64 / CH, N = 32 / RPL;   // chunks a row, rows a load, loads
+// Loads ROWS keys of the list from n0 on into LDS rows (1024 bytes a load: 64 lanes x
+// 16; ROWS a multiple of 16, the period of the swizzles). Whole runs of the window go
+// from a uniform base; those that hold sinks or end behind the list from each lane's
+// own row, the list's last key standing for those behind it (their probabilities are
+// 0).
+template <int D, bool IS_V, int ROWS>
+__device__ __forceinline__ void stage_rows(uint32_t lds, const uint16_t* base, int64_t stride,
+                                           const Span& sp, int32_t n0, int lane) {
+  constexpr int CH = D / 8, RPL = 64 / CH, N = ROWS / RPL;   // chunks a row, rows a load, loads
   const int r = lane / CH, pc = lane % CH;
-  if (n0 >= sp.sinks && n0 + 32 <= sp.total) {
+  if (n0 >= sp.sinks && n0 + ROWS <= sp.total) {
     const char* b = scalar_base(base + (int64_t)(n0 + sp.shift) * stride);
     const uint32_t row = (uint32_t)r * (uint32_t)stride * 2u;
 #pragma unroll
@@ -165,15 +166,17 @@ struct RowAcc {
   float sum, m;
 };
 
-// The scores of one block to the probabilities (16-bit pairs of keys as they
-// lie), raising M and rescaling what is accumulated where the max asks for it.
-template <int DT, int MODE, int D>
-__device__ __forceinline__ void softmax_block(const f32x16& s, float c0, RowAcc<D>& acc,
-                                              u32x4 (&p)[2]) {
+// The scores of NB blocks to probabilities (16-bit pairs of keys as they lie), raising
+// M and rescaling what is accumulated where the max asks for it.
+template <int DT, int MODE, int D, int NB>
+__device__ __forceinline__ void softmax_blocks(const f32x16 (&s)[NB], float c0, RowAcc<D>& acc,
+                                               u32x4 (&p)[2 * NB]) {
   constexpr float kScale = MODE == EXACT ? 1.0f : 0x1p-23f;
-  float top = s[0];
+  float top = s[0][0];
 #pragma unroll
-  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
   top = fmaxf(top, other_half(top)) * (c0 * kScale);
   if (__any(top > acc.m + kLazy)) {
     const float m = top > acc.m + kLazy ? __builtin_ceilf(top) : acc.m;
@@ -187,16 +190,34 @@ __device__ __forceinline__ void softmax_block(const f32x16& s, float c0, RowAcc<
   }
   const float c1 = MODE == EXACT ? -acc.m : (127.0f - acc.m) * 0x1p23f;
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    float e[4];
+  for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      e[i] = qexp_row<MODE, true>(s[4 * g + i], c0, c1);
-      acc.sum += e[i];
+    for (int g = 0; g < 4; ++g) {
+      float e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[i] = qexp_row<MODE, true>(s[b][4 * g + i], c0, c1);
+        acc.sum += e[i];
+      }
+      p[2 * b + (g >> 1)][2 * (g & 1)] = wpack<DT>(e[0], e[1]);
+      p[2 * b + (g >> 1)][2 * (g & 1) + 1] = wpack<DT>(e[2], e[3]);
     }
-    p[g >> 1][2 * (g & 1)] = wpack<DT>(e[0], e[1]);
-    p[g >> 1][2 * (g & 1) + 1] = wpack<DT>(e[2], e[3]);
-  }
+}
+
+// whether rows at positions first .. last see all of N keys of the list
+template <int N>
+__device__ __forceinline__ bool all_seen(const Span& sp, int32_t n0, int32_t first, int32_t last,
+                                         const WindowArgs& g) {
+  const int32_t a = sp.key(n0), z = sp.key(n0 + N - 1);
+  return z <= first && z - a == N - 1 && ((uint32_t)z < g.sinks || (uint32_t)(last - a) < g.window);
+}
+// whether they see none of them (of a run without a gap)
+template <int N>
+__device__ __forceinline__ bool none_seen(const Span& sp, int32_t n0, int32_t first, int32_t last,
+                                          const WindowArgs& g) {
+  const int32_t a = sp.key(n0), z = sp.key(n0 + N - 1);
+  return a > last || (z - a == N - 1 && (uint32_t)a >= g.sinks && first > z &&
+                      (uint32_t)(first - z) >= g.window);
 }
 
 // -inf for the keys of block n0 that the row at `pos` does not see
@@ -256,8 +277,8 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
   const uint32_t lds =
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf + wave * kWave;
   auto load = [&](int32_t n, int slot) {
-    stage_block<D, false>(lds + 2 * kBlk * slot, K, g.ks, sp, 32 * n, lane);
-    stage_block<D, true>(lds + 2 * kBlk * slot + kBlk, V, g.vs, sp, 32 * n, lane);
+    stage_rows<D, false, 32>(lds + 2 * kBlk * slot, K, g.ks, sp, 32 * n, lane);
+    stage_rows<D, true, 32>(lds + 2 * kBlk * slot + kBlk, V, g.vs, sp, 32 * n, lane);
   };
 
   RowAcc<D> acc;
@@ -275,16 +296,12 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
       wait_loads<0>();
     }
     const char* kblk = buf + 2 * kBlk * slot;
-    f32x16 s = {};
+    f32x16 s[1] = {};
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s = wmma<DT>(read_k<D>(kblk, fr, h, ks), qf[ks], s);
-    // every key of the block seen by every row of the tile: no mask
-    const int32_t ka = sp.key(32 * n), kz = sp.key(32 * n + 31);
-    const bool all = kz <= first && (kz - ka == 31) &&
-                     ((uint32_t)kz < g.sinks || (uint32_t)(last - ka) < g.window);
-    if (!all) mask_block(s, sp, 32 * n, pos, h, g);
+    for (int ks = 0; ks < D / 16; ++ks) s[0] = wmma<DT>(read_k<D>(kblk, fr, h, ks), qf[ks], s[0]);
+    if (!all_seen<32>(sp, 32 * n, first, last, g)) mask_block(s[0], sp, 32 * n, pos, h, g);
     u32x4 p[2];
-    softmax_block<DT, MODE, D>(s, g.c0, acc, p);
+    softmax_blocks<DT, MODE, D>(s, g.c0, acc, p);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -352,6 +369,138 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
   }
 }
 
+// 128 rows in one workgroup, 32 a wave, which share tiles of 64 keys in LDS: a tile is
+// multiplied while the next one is on its way, with one barrier a tile. What bounds it
+// is the matrix cores beside the exponentials' VALU work; two workgroups share a
+// compute unit, so that one wave's products run under another's exponentials.
+constexpr int kManyKeys = 64;
+
+template <int DT, int MODE, int D>
+__global__ __launch_bounds__(64 * kWinWaves, 2) void window_many_kernel(WindowArgs g) {
+  constexpr int kTile = 2 * kManyKeys * D;          // bytes of K or V of a tile
+  constexpr int kRows = kManyKeys / kWinWaves;      // a wave loads
+  __shared__ __attribute__((aligned(16))) char s_buf[4 * kTile];   // K and V, two buffers
+
+  const int lane = threadIdx.x & 63, fr = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Workgroups go round the 8 XCDs: each XCD gets consecutive tiles, which share
+  // most of their keys, for its own L2.
+  const uint32_t x = blockIdx.x & 7u, per = gridDim.x >> 3, rest = gridDim.x & 7u;
+  const uint32_t id = x * per + min(x, rest) + (blockIdx.x >> 3);
+  const int split = id % (uint32_t)g.nsplit;
+  const uint32_t item = id / (uint32_t)g.nsplit;
+  const uint32_t tiles = ((uint32_t)g.tiles + kWinWaves - 1) / kWinWaves;
+  const int tile = item % tiles;
+  const uint32_t bh = item / tiles;
+  const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
+  const int32_t qlen = seq_len(g.q_lens, b, g.sq), kvlen = seq_len(g.kv_lens, b, g.skv);
+  const int32_t rows = qlen * g.group, r0 = 32 * kWinWaves * tile;
+  if (r0 >= rows) return;
+  const int32_t off = kvlen - qlen;
+  const Span sp(off + r0 / g.group, off + min(r0 + 32 * kWinWaves - 1, rows - 1) / g.group, g);
+  const int32_t steps = (sp.total + kManyKeys - 1) / kManyKeys;
+  const int32_t n_lo = (int32_t)((int64_t)steps * split / g.nsplit);
+  const int32_t n_hi = (int32_t)((int64_t)steps * (split + 1) / g.nsplit);
+  // this wave's rows (past the last row: that row again, not stored)
+  const int32_t w0 = r0 + 32 * wave;
+  const int32_t row = min(w0 + fr, rows - 1);
+  const int32_t query = row / g.group, head = hk * g.group + row % g.group;
+  const int32_t pos = off + query;
+  const int32_t first = off + min(w0, rows - 1) / g.group;
+  const int32_t last = off + min(w0 + 31, rows - 1) / g.group;
+
+  u32x4 qf[D / 16];
+  {
+    const uint16_t* qr = g.q + b * g.qb + query * g.qs + head * g.qh + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(qr + 16 * ks);
+  }
+  const uint16_t* K = g.k + b * g.kb + hk * g.kh;
+  const uint16_t* V = g.v + b * g.vb + hk * g.vh;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf +
+                       wave * kRows * 2 * D;
+  auto load = [&](int32_t n, int slot) {
+    stage_rows<D, false, kRows>(lds + 2 * kTile * slot, K, g.ks, sp, kManyKeys * n + kRows * wave, lane);
+    stage_rows<D, true, kRows>(lds + 2 * kTile * slot + kTile, V, g.vs, sp,
+                               kManyKeys * n + kRows * wave, lane);
+  };
+
+  RowAcc<D> acc;
+  acc.sum = 0.0f;
+  acc.m = kNoMax;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) acc.o[d] = f32x16{};
+  if (n_lo < n_hi) load(n_lo, 0);
+  int slot = 0;
+  for (int32_t n = n_lo; n < n_hi; ++n, slot ^= 1) {
+    wait_loads<0>();
+    __syncthreads();   // the tile is there, and nobody reads the other buffer
+    if (n + 1 < n_hi) load(n + 1, slot ^ 1);
+    const int32_t n0 = kManyKeys * n;
+    if (none_seen<kManyKeys>(sp, n0, first, last, g)) continue;
+    const char* kt = s_buf + 2 * kTile * slot;
+    f32x16 s[2] = {};
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+        s[c] = wmma<DT>(read_k<D>(kt + 64 * D * c, fr, h, ks), qf[ks], s[c]);
+    if (!all_seen<kManyKeys>(sp, n0, first, last, g)) {
+      mask_block(s[0], sp, n0, pos, h, g);
+      mask_block(s[1], sp, n0 + 32, pos, h, g);
+    }
+    u32x4 p[4];
+    softmax_blocks<DT, MODE, D>(s, g.c0, acc, p);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+        acc.o[d] = wmma<DT>(read_v<D>(kt + kTile, lane, ks, d), p[ks], acc.o[d]);
+  }
+
+  const float sum = acc.sum + other_half(acc.sum);
+  if (g.nsplit > 1) {
+    if (w0 >= rows) return;
+    const int64_t slot32 = ((int64_t)bh * g.tiles + kWinWaves * tile + wave) * g.nsplit + split;
+    float* w = g.ws + slot32 * (64 + 32 * D);
+    if (h == 0) {
+      w[fr] = acc.m;
+      w[32 + fr] = sum;
+    }
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(w + 64 + fr * D + 32 * d + 8 * i + 4 * h) =
+            float4{acc.o[d][4 * i], acc.o[d][4 * i + 1], acc.o[d][4 * i + 2], acc.o[d][4 * i + 3]};
+    return;
+  }
+  // Rows of the output through LDS (the wave's own rows, chunks swizzled as K's), so
+  // that whole rows are stored 16 bytes a lane.
+  __syncthreads();
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  char* ow = s_buf + wave * 64 * D;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x2 w = {wpack<DT>(acc.o[d][4 * i] * inv, acc.o[d][4 * i + 1] * inv),
+                       wpack<DT>(acc.o[d][4 * i + 2] * inv, acc.o[d][4 * i + 3] * inv)};
+      *reinterpret_cast<u32x2*>(ow + fr * 2 * D + 16 * ((4 * d + i) ^ kswizzle<D>(fr)) + 8 * h) = w;
+    }
+  __builtin_amdgcn_wave_barrier();
+  wait_lds();
+  constexpr int CH = D / 8, RPL = 64 / CH;
+#pragma unroll
+  for (int j = 0; j < 32 / RPL; ++j) {
+    const int r = RPL * j + lane / CH, c = lane % CH;
+    if (w0 + r >= rows) continue;
+    const int32_t qi = (w0 + r) / g.group, hd = hk * g.group + (w0 + r) % g.group;
+    *reinterpret_cast<u32x4*>(g.o + b * g.ob + qi * g.os + hd * g.oh + 8 * c) =
+        *reinterpret_cast<const u32x4*>(ow + r * 2 * D + 16 * (c ^ kswizzle<D>(r)));
+  }
+}
+
 // Joins the splits of a tile: thread t takes D / 8 dims of row t / 8.
 template <int DT, int D>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs g) {
@@ -395,21 +544,26 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs g) {
 // Host side
 // ---------------------------------------------------------------------------
 struct WindowPlan {
-  int64_t tiles;    // row tiles of a key head
+  int64_t tiles;    // tiles of 32 rows of a key head
   int64_t nsplit;   // workgroups that share a tile's keys
+  bool many;        // 128 rows a workgroup
 };
 
 // Splits: few tiles leave compute units idle while each walks a long window, so a
 // tile's keys go to as many workgroups as bring the launch to kWinTarget, with at
-// least 8 blocks of 32 keys (two a wave) for each.
+// least 256 keys for each.
 constexpr int64_t kWinTarget = 512;
+constexpr int64_t kManyRows = 96;   // rows from which on 128 share a workgroup
 
 static WindowPlan window_plan(int64_t batch, int64_t sq, int64_t skv, int64_t group,
                               int64_t kv_heads, int64_t window, int64_t sinks) {
   WindowPlan p;
-  p.tiles = (sq * group + 31) / 32;
-  const int64_t items = batch * kv_heads * p.tiles;
-  const int64_t queries = (31 + group) / group;   // most positions a tile covers, less one
+  const int64_t rows = sq * group;
+  p.tiles = (rows + 31) / 32;
+  p.many = rows >= kManyRows;
+  const int64_t wide = p.many ? 128 : 32;
+  const int64_t items = batch * kv_heads * ((rows + wide - 1) / wide);
+  const int64_t queries = (wide - 1 + group) / group;   // most positions a tile covers, less one
   const int64_t keys = std::min(skv, std::min(window, skv) + std::min(sinks, skv) + queries);
   const int64_t most = (keys + 255) / 256;
   p.nsplit = items == 0 ? 1 : std::max<int64_t>(1, std::min(most, kWinTarget / items));
@@ -432,17 +586,26 @@ static bool window_shape_ok(int64_t batch, int64_t sq, int64_t skv, int64_t head
   return batch * kv_heads * ((sq * (heads / kv_heads) + 31) / 32) <= (1 << 24);
 }
 
-template <int DT, int D>
-static void launch_window(int mode, dim3 grid, hipStream_t s, const WindowArgs& g) {
-  const dim3 block(64 * kWinWaves);
-  switch (mode) {
-    case QUAKE_EXACT: hipLaunchKernelGGL((window_few_kernel<DT, EXACT, D>), grid, block, 0, s, g); break;
-    case QUAKE_1: hipLaunchKernelGGL((window_few_kernel<DT, Q1, D>), grid, block, 0, s, g); break;
-    case QUAKE_2: hipLaunchKernelGGL((window_few_kernel<DT, Q2, D>), grid, block, 0, s, g); break;
-    default: hipLaunchKernelGGL((window_few_kernel<DT, Q2M, D>), grid, block, 0, s, g); break;
-  }
+template <int DT, int MODE, int D>
+static void launch_window(bool many, int64_t heads, hipStream_t s, const WindowArgs& g) {
+  const int64_t wide = many ? kWinWaves : 1;   // tiles of 32 rows a workgroup
+  const dim3 grid((uint32_t)(heads * ((g.tiles + wide - 1) / wide) * g.nsplit));
+  if (many)
+    hipLaunchKernelGGL((window_many_kernel<DT, MODE, D>), grid, dim3(64 * kWinWaves), 0, s, g);
+  else
+    hipLaunchKernelGGL((window_few_kernel<DT, MODE, D>), grid, dim3(64 * kWinWaves), 0, s, g);
   if (g.nsplit > 1)
-    hipLaunchKernelGGL((window_join_kernel<DT, D>), dim3(grid.x / g.nsplit), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((window_join_kernel<DT, D>), dim3((uint32_t)(heads * g.tiles)), dim3(256), 0,
+                       s, g);
+}
+template <int DT, int D>
+static void launch_window(int mode, bool many, int64_t heads, hipStream_t s, const WindowArgs& g) {
+  switch (mode) {
+    case QUAKE_EXACT: launch_window<DT, EXACT, D>(many, heads, s, g); break;
+    case QUAKE_1: launch_window<DT, Q1, D>(many, heads, s, g); break;
+    case QUAKE_2: launch_window<DT, Q2, D>(many, heads, s, g); break;
+    default: launch_window<DT, Q2M, D>(many, heads, s, g); break;
+  }
 }
 
 }  // namespace qk
@@ -517,14 +680,14 @@ extern "C" quake_status quake_attention_window(
   g.window = (uint32_t)window;
   g.sinks = (uint32_t)sinks;
   g.c0 = c0;
-  const dim3 grid((uint32_t)(batch * kv_heads * p.tiles * g.nsplit));
+  const int64_t kvh = batch * kv_heads;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == QUAKE_BF16) {
-    if (dim == 64) launch_window<BF16, 64>(mode, grid, s, g);
-    else launch_window<BF16, 128>(mode, grid, s, g);
+    if (dim == 64) launch_window<BF16, 64>(mode, p.many, kvh, s, g);
+    else launch_window<BF16, 128>(mode, p.many, kvh, s, g);
   } else {
-    if (dim == 64) launch_window<F16, 64>(mode, grid, s, g);
-    else launch_window<F16, 128>(mode, grid, s, g);
+    if (dim == 64) launch_window<F16, 64>(mode, p.many, kvh, s, g);
+    else launch_window<F16, 128>(mode, p.many, kvh, s, g);
   }
   return launch_status();
 }
