@@ -31,6 +31,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "quake_device.hpp"
 #include "quake_host.hpp"
@@ -70,6 +71,23 @@ __device__ __forceinline__ f32x16 wmma(u32x4 a, u32x4 b, f32x16 c) {
 template <int DT>
 __device__ __forceinline__ uint32_t wpack(float a, float b) {
   return DT == BF16 ? pack_bf16(a, b) : pack_f16(a, b);
+}
+// The loads of v done here: waited for at their first use, inside the loop, they would
+// be waited for there every time, and with them the keys on their way to LDS.
+template <int N>
+__device__ __forceinline__ void settle(u32x4 (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+// a + the sum of a pair, of its rounded values
+template <int DT>
+__device__ __forceinline__ float wsum(uint32_t pair, float a) {
+  if constexpr (DT == BF16)
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair),
+                                           bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, a, false);
+  else
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pair),
+                                  f16x2_t{(_Float16)1.0f, (_Float16)1.0f}, a, false);
 }
 __device__ __forceinline__ float other_half(float v) {   // the value of lane l xor 32
   const auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
@@ -166,58 +184,53 @@ struct RowAcc {
   float sum, m;
 };
 
-// The scores of NB blocks to probabilities (16-bit pairs of keys as they lie), raising
-// M and rescaling what is accumulated where the max asks for it.
-template <int DT, int MODE, int D, int NB>
-__device__ __forceinline__ void softmax_blocks(const f32x16 (&s)[NB], float c0, RowAcc<D>& acc,
-                                               u32x4 (&p)[2 * NB]) {
-  constexpr float kScale = MODE == EXACT ? 1.0f : 0x1p-23f;
-  float top = s[0][0];
+// the larger of the row's scores in a block, in base-2 units
+template <int MODE>
+__device__ __forceinline__ float block_top(const f32x16& s, float c0) {
+  float top = s[0];
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+  return fmaxf(top, other_half(top)) * (c0 * (MODE == EXACT ? 1.0f : 0x1p-23f));
+}
+// M raised to `top` where that is more than `lazy` above it, and what is accumulated
+// rescaled; returns the exponent it was rescaled by.
+template <int D>
+__device__ __forceinline__ int32_t raise_max(float top, float lazy, RowAcc<D>& acc) {
+  const float m = top > acc.m + lazy ? __builtin_ceilf(top) : acc.m;
+  const int32_t e = down_shift(acc.m, m);
+  acc.m = m;
+  acc.sum = __builtin_amdgcn_ldexpf(acc.sum, e);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
-  top = fmaxf(top, other_half(top)) * (c0 * kScale);
-  if (__any(top > acc.m + kLazy)) {
-    const float m = top > acc.m + kLazy ? __builtin_ceilf(top) : acc.m;
-    const int32_t e = down_shift(acc.m, m);
-    acc.m = m;
-    acc.sum = __builtin_amdgcn_ldexpf(acc.sum, e);
+  for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc.o[d][r] = __builtin_amdgcn_ldexpf(acc.o[d][r], e);
-  }
-  const float c1 = MODE == EXACT ? -acc.m : (127.0f - acc.m) * 0x1p23f;
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      float e[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e[i] = qexp_row<MODE, true>(s[b][4 * g + i], c0, c1);
-        acc.sum += e[i];
-      }
-      p[2 * b + (g >> 1)][2 * (g & 1)] = wpack<DT>(e[0], e[1]);
-      p[2 * b + (g >> 1)][2 * (g & 1) + 1] = wpack<DT>(e[2], e[3]);
-    }
+    for (int r = 0; r < 16; ++r) acc.o[d][r] = __builtin_amdgcn_ldexpf(acc.o[d][r], e);
+  return e;
+}
+// a 16-bit pair times 2^e
+template <int DT>
+__device__ __forceinline__ uint32_t scale_pair(uint32_t p, int32_t e) {
+  const float a = DT == BF16 ? bf16_lo(p) : f16_lo(p), b = DT == BF16 ? bf16_hi(p) : f16_hi(p);
+  return wpack<DT>(__builtin_amdgcn_ldexpf(a, e), __builtin_amdgcn_ldexpf(b, e));
+}
+template <int MODE>
+__device__ __forceinline__ float row_c1(float m) {
+  return MODE == EXACT ? -m : (127.0f - m) * 0x1p23f;
+}
+// Scores r, r + 1 to a pair of probabilities, added to the sum as rounded: numerator
+// and denominator then share the rounding.
+template <int DT, int MODE>
+__device__ __forceinline__ uint32_t prob_pair(const f32x16& s, int r, float c0, float c1, float& sum) {
+  const uint32_t p = wpack<DT>(qexp_row<MODE, true>(s[r], c0, c1),
+                               qexp_row<MODE, true>(s[r + 1], c0, c1));
+  sum = wsum<DT>(p, sum);
+  return p;
 }
 
-// whether rows at positions first .. last see all of N keys of the list
-template <int N>
+// whether rows at positions first .. last see all of 32 keys of the list
 __device__ __forceinline__ bool all_seen(const Span& sp, int32_t n0, int32_t first, int32_t last,
                                          const WindowArgs& g) {
-  const int32_t a = sp.key(n0), z = sp.key(n0 + N - 1);
-  return z <= first && z - a == N - 1 && ((uint32_t)z < g.sinks || (uint32_t)(last - a) < g.window);
-}
-// whether they see none of them (of a run without a gap)
-template <int N>
-__device__ __forceinline__ bool none_seen(const Span& sp, int32_t n0, int32_t first, int32_t last,
-                                          const WindowArgs& g) {
-  const int32_t a = sp.key(n0), z = sp.key(n0 + N - 1);
-  return a > last || (z - a == N - 1 && (uint32_t)a >= g.sinks && first > z &&
-                      (uint32_t)(first - z) >= g.window);
+  const int32_t a = sp.key(n0), z = sp.key(n0 + 31);
+  return z <= first && z - a == 31 && ((uint32_t)z < g.sinks || (uint32_t)(last - a) < g.window);
 }
 
 // -inf for the keys of block n0 that the row at `pos` does not see
@@ -271,6 +284,7 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(qr + 16 * ks);
   }
+  settle(qf);
   const uint16_t* K = g.k + b * g.kb + hk * g.kh;
   const uint16_t* V = g.v + b * g.vb + hk * g.vh;
   char* buf = s_buf + wave * kWave;
@@ -296,12 +310,17 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
       wait_loads<0>();
     }
     const char* kblk = buf + 2 * kBlk * slot;
-    f32x16 s[1] = {};
+    f32x16 s = {};
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s[0] = wmma<DT>(read_k<D>(kblk, fr, h, ks), qf[ks], s[0]);
-    if (!all_seen<32>(sp, 32 * n, first, last, g)) mask_block(s[0], sp, 32 * n, pos, h, g);
+    for (int ks = 0; ks < D / 16; ++ks) s = wmma<DT>(read_k<D>(kblk, fr, h, ks), qf[ks], s);
+    if (!all_seen(sp, 32 * n, first, last, g)) mask_block(s, sp, 32 * n, pos, h, g);
+    const float top = block_top<MODE>(s, g.c0);
+    if (__any(top > acc.m + kLazy)) raise_max(top, kLazy, acc);
+    const float c1 = row_c1<MODE>(acc.m);
     u32x4 p[2];
-    softmax_blocks<DT, MODE, D>(s, g.c0, acc, p);
+#pragma unroll
+    for (int r = 0; r < 16; r += 2)
+      p[r >> 3][(r >> 1) & 3] = prob_pair<DT, MODE>(s, r, g.c0, c1, acc.sum);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -369,10 +388,15 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
   }
 }
 
-// 128 rows in one workgroup, 32 a wave, which share tiles of 64 keys in LDS: a tile is
-// multiplied while the next one is on its way, with one barrier a tile. What bounds it
-// is the matrix cores beside the exponentials' VALU work; two workgroups share a
-// compute unit, so that one wave's products run under another's exponentials.
+// 128 rows in one workgroup, 32 a wave, which share tiles of 64 keys in LDS (two
+// blocks of 32; two tiles each of K and V). A wave's products run under its own VALU
+// work: while block n's scores become probabilities, the scores of block n + 1 and the
+// second product of block n - 1 are computed, one product of each with every 512 / D
+// of the block's 16 values a lane. One barrier a tile, between its blocks: by then K
+// of the next tile and V of this one have landed, and K of this one and V of the last
+// are done with, so the loads of two tiles on start there.
+// What bounds it is VALU issue, so whether M has to rise is asked of each lane's own
+// scores; only if so are the two halves of a row brought together.
 constexpr int kManyKeys = 64;
 
 template <int DT, int MODE, int D>
@@ -415,14 +439,17 @@ __global__ __launch_bounds__(64 * kWinWaves, 2) void window_many_kernel(WindowAr
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *reinterpret_cast<const u32x4*>(qr + 16 * ks);
   }
+  settle(qf);
   const uint16_t* K = g.k + b * g.kb + hk * g.kh;
   const uint16_t* V = g.v + b * g.vb + hk * g.vh;
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf +
                        wave * kRows * 2 * D;
-  auto load = [&](int32_t n, int slot) {
-    stage_rows<D, false, kRows>(lds + 2 * kTile * slot, K, g.ks, sp, kManyKeys * n + kRows * wave, lane);
-    stage_rows<D, true, kRows>(lds + 2 * kTile * slot + kTile, V, g.vs, sp,
-                               kManyKeys * n + kRows * wave, lane);
+  auto load_k = [&](int32_t t) {
+    stage_rows<D, false, kRows>(lds + kTile * ((t - n_lo) & 1), K, g.ks, sp, kManyKeys * t + kRows * wave, lane);
+  };
+  auto load_v = [&](int32_t t) {
+    stage_rows<D, true, kRows>(lds + kTile * (2 + ((t - n_lo) & 1)), V, g.vs, sp, kManyKeys * t + kRows * wave,
+                               lane);
   };
 
   RowAcc<D> acc;
@@ -430,32 +457,126 @@ __global__ __launch_bounds__(64 * kWinWaves, 2) void window_many_kernel(WindowAr
   acc.m = kNoMax;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) acc.o[d] = f32x16{};
-  if (n_lo < n_hi) load(n_lo, 0);
-  int slot = 0;
-  for (int32_t n = n_lo; n < n_hi; ++n, slot ^= 1) {
-    wait_loads<0>();
-    __syncthreads();   // the tile is there, and nobody reads the other buffer
-    if (n + 1 < n_hi) load(n + 1, slot ^ 1);
-    const int32_t n0 = kManyKeys * n;
-    if (none_seen<kManyKeys>(sp, n0, first, last, g)) continue;
-    const char* kt = s_buf + 2 * kTile * slot;
-    f32x16 s[2] = {};
+  // tiles of which this wave's rows may see something, and of which they see all
+  const int32_t seen = last < 0 ? 0 : last + 1 - (last < sp.sinks ? 0 : sp.shift);
+  const int32_t t_hi = min(n_hi, (seen + kManyKeys - 1) / kManyKeys);
+  int32_t t_lo = n_lo;
+  const int32_t low = (uint32_t)last >= g.window ? last - (int32_t)g.window + 1 : 0;   // seen by all
+  const int32_t all_lo = (max(low - sp.shift, sp.sinks) + kManyKeys - 1) / kManyKeys;
+  const int32_t all_hi = first < 0 ? 0 : max(first + 1 - sp.shift, 0) / kManyKeys;
+  if (g.sinks == 0 && first >= 0 && (uint32_t)first >= g.window)
+    t_lo = max(t_lo, (first - (int32_t)g.window + 1 - sp.shift) / kManyKeys);
+
+  constexpr int NU = D / 16, NE = 16 / NU;   // products of a kind a block; values for each
+  constexpr int ND = D / 32;
+  // Where this lane reads its operands in block 0: K's chunk of step ks, V's of dims
+  // 32 d on; other blocks and keys at constant distances.
+  typedef __attribute__((address_space(3))) const char* lds_ptr;
+  lds_ptr kat[NU], vat[ND];
+  {
+    const lds_ptr base = (lds_ptr)s_buf;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int ks = 0; ks < NU; ++ks)
+      kat[ks] = base + fr * (2 * D) + 16 * ((2 * ks + h) ^ kswizzle<D>(fr));
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-        s[c] = wmma<DT>(read_k<D>(kt + 64 * D * c, fr, h, ks), qf[ks], s[c]);
-    if (!all_seen<kManyKeys>(sp, n0, first, last, g)) {
-      mask_block(s[0], sp, n0, pos, h, g);
-      mask_block(s[1], sp, n0 + 32, pos, h, g);
+    for (int d = 0; d < ND; ++d) {
+      const int r = 4 * h + ((lane >> 2) & 3);
+      const int c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+      vat[d] = base + 2 * kTile + r * (2 * D) + 16 * (c ^ vswizzle<D>(r)) + 8 * (lane & 1);
     }
-    u32x4 p[4];
-    softmax_blocks<DT, MODE, D>(s, g.c0, acc, p);
+  }
+  auto get_k = [&](int blk, int ks) {
+    return *(__attribute__((address_space(3))) const u32x4*)(kat[ks] + 64 * D * blk);
+  };
+  auto get_v = [&](int blk, int u) {   // of product u: keys 16 (u / ND) on, dims 32 (u mod ND) on
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const lds_ptr a = vat[u % ND] + 64 * D * blk + 32 * D * (u / ND);
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)a));
+    const u32x2 hi = __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(a + 16 * D)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  };
+  const float units = g.c0 * (MODE == EXACT ? 1.0f : 0x1p-23f);
+  float limit = -INFINITY;   // scores up to here leave M as it is
+  // Block n (scores s, in LDS block KN - 1) while the scores of block n + 1 (KN) go to
+  // sn; pp: the probabilities of block n - 1, whose values lie in block VP; pn: block
+  // n's.
+  auto step = [&](int32_t n, bool plain, auto kn, auto vp, f32x16& s, f32x16& sn, u32x4 (&pp)[2],
+                  u32x4 (&pn)[2]) {
+    constexpr int KN = decltype(kn)::value, VP = decltype(vp)::value;
+    u32x4 ka[NU], va[NU];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
+    for (int u = 0; u < 2; ++u) {
+      ka[u] = get_k(KN, u);
+      va[u] = get_v(VP, u);
+    }
+    if (!plain) mask_block(s, sp, 32 * n, pos, h, g);
+    float top = s[0];
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-        acc.o[d] = wmma<DT>(read_v<D>(kt + kTile, lane, ks, d), p[ks], acc.o[d]);
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    if (__any(top > limit)) {
+      const int32_t e = raise_max(fmaxf(top, other_half(top)) * units, kLazy, acc);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pp[i >> 2][i & 3] = scale_pair<DT>(pp[i >> 2][i & 3], e);
+      limit = (acc.m + kLazy) / units;
+    }
+    const float c1 = row_c1<MODE>(acc.m);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      if (u + 2 < NU) {
+        ka[u + 2] = get_k(KN, u + 2);
+        va[u + 2] = get_v(VP, u + 2);
+      }
+      const f32x16 zero = {};
+      sn = wmma<DT>(ka[u], qf[u], u == 0 ? zero : sn);
+      acc.o[u % ND] = wmma<DT>(va[u], pp[u / ND], acc.o[u % ND]);
+#pragma unroll
+      for (int r = NE * u; r < NE * u + NE; r += 2)
+        pn[r >> 3][(r >> 1) & 3] = prob_pair<DT, MODE>(s, r, g.c0, c1, acc.sum);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  u32x4 pa[2], pb[2];
+  f32x16 sa, sb;
+  auto two_blocks = [&](int32_t t, auto parity) {
+    constexpr int B = 2 * decltype(parity)::value;   // the tile's first block in LDS
+    const bool mine = t >= t_lo && t < t_hi, plain = t >= all_lo && t < all_hi;
+    if (mine && t == t_lo) {
+      sa = f32x16{};
+#pragma unroll
+      for (int u = 0; u < NU; ++u) sa = wmma<DT>(get_k(B, u), qf[u], sa);
+      pb[0] = pb[1] = u32x4{0u, 0u, 0u, 0u};   // no block before
+    }
+    if (mine)
+      step(2 * t, plain, std::integral_constant<int, B + 1>{}, std::integral_constant<int, 3 - B>{},
+           sa, sb, pb, pa);
+    wait_lds();
+    wait_loads<0>();
+    __syncthreads();
+    if (t + 2 < n_hi) load_k(t + 2);
+    if (t + 1 < n_hi) load_v(t + 1);
+    if (!mine) return;
+    step(2 * t + 1, plain, std::integral_constant<int, 2 - B>{}, std::integral_constant<int, B>{}, sb,
+         sa, pa, pb);
+    if (t + 1 == t_hi) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+        acc.o[u % ND] = wmma<DT>(get_v(B + 1, u), pb[u / ND], acc.o[u % ND]);
+    }
+  };
+  if (n_lo < n_hi) {
+    // V of the tile before the first is read (times 0): K's rows, which are finite
+    // where K is
+    stage_rows<D, false, kRows>(lds + kTile * 3, K, g.ks, sp, kManyKeys * n_lo + kRows * wave, lane);
+    load_k(n_lo);
+    load_v(n_lo);
+    if (n_lo + 1 < n_hi) load_k(n_lo + 1);
+    wait_loads<0>();
+    __syncthreads();
+  }
+  for (int32_t t = n_lo; t < n_hi; t += 2) {
+    two_blocks(t, std::integral_constant<int, 0>{});
+    if (t + 1 < n_hi) two_blocks(t + 1, std::integral_constant<int, 1>{});
   }
 
   const float sum = acc.sum + other_half(acc.sum);

@@ -49,7 +49,9 @@ def window_attention(q, k, v, window, sinks, mode, t, q_lens=None, kv_lens=None)
     units, an exponential then by that plus ARG relative (both sides of the
     quotient: twice), its 16-bit rounding by half a step (binary16: at least 2^-25
     against a sum of at least 1/2), the products and sums by (keys + 8) 2^-24 each,
-    the result by half a step of its format."""
+    the result by half a step of its format. The sum is of the rounded p too: with
+    p' = p (1 + e), sum p' v / sum p' - o = sum p' e' (v - o) / sum p', so the rounding
+    costs half a step of mean |v| + |o|, not of mean |v| alone."""
     dt = q.dtype
     b, sq, h, d = q.shape
     skv, hk = k.shape[1], k.shape[2]
@@ -84,7 +86,7 @@ def window_attention(q, k, v, window, sinks, mode, t, q_lens=None, kv_lens=None)
         o[:, :, n] = torch.matmul(p, vv) * inv
         mean = torch.matmul(p, vv.abs()) * inv
         rel = 2 * off + 2 * jump(mode) + eps / 2 + 2 * (keys + 8) * 2.0 ** -24
-        bound[:, :, n] = 1.01 * (mean * rel + o[:, :, n].abs() * eps / 2)
+        bound[:, :, n] = 1.01 * (mean * rel + 2 * o[:, :, n].abs() * eps / 2)
         if dt == torch.float16:
             bound[:, :, n] += torch.matmul(seen.double(), vv.abs()) * (2.0 ** -25) * 2 * inv.clamp(max=2.0)
             bound[:, :, n] += 2.0 ** -25
