@@ -66,11 +66,11 @@ struct Sum {
   }
 };
 
-template <int DT, int MODE>
-__device__ __forceinline__ void add_values(const float* f, int n, float c0, Sum& a) {
+template <int MODE, int N>
+__device__ __forceinline__ void add_values(const float (&f)[N], float c0, Sum& a) {
   float top = f[0];
 #pragma unroll
-  for (int k = 1; k < n; ++k) top = fmaxf(top, f[k]);
+  for (int k = 1; k < N; ++k) top = fmaxf(top, f[k]);
   top *= c0 * kToUnits<MODE>;
   if (top > a.M) {
     const float M = __builtin_ceilf(top);
@@ -80,33 +80,49 @@ __device__ __forceinline__ void add_values(const float* f, int n, float c0, Sum&
   const float c1 = c1_of<MODE>(a.M);
   float s[4] = {};
 #pragma unroll
-  for (int k = 0; k < n; ++k) s[k & 3] += qexp_row<MODE, true>(f[k], c0, c1);
+  for (int k = 0; k < N; ++k) s[k & 3] += qexp_row<MODE, true>(f[k], c0, c1);
   a.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
 }
 
-// Statistics of vectors [a, z) of a row by the workgroup.
+// Vectors of [a, z) that lie inside the row as a whole; the row's first and last are
+// taken by one thread each.
+template <int DT>
+struct Inner {
+  uint32_t a, z;
+  bool head, tail;
+  __device__ __forceinline__ Inner(const RowVecs<DT>& r, uint32_t a_, uint32_t z_)
+      : a(max(a_, 1u)), z(min(z_, r.n - 1u)), head(a_ == 0 && z_ > 0 && threadIdx.x == 0),
+        tail(z_ == r.n && r.n > 1u && a_ < z_ && threadIdx.x == 64) {}
+};
+
+// Statistics of vectors [a, z) of a row by the workgroup: values four vectors at a
+// time (one max, one binary64 addition).
 template <int DT, int MODE>
 __device__ __forceinline__ Sum row_sum(const RowVecs<DT>& r, uint32_t a, uint32_t z, float c0) {
   constexpr int V = kV<DT>, U = 4;
+  const Inner<DT> in(r, a, z);
   Sum acc;
-  uint32_t i = a + threadIdx.x;
-  for (; i + (U - 1) * kDsThreads < z; i += U * kDsThreads) {
+  uint32_t i = in.a + threadIdx.x;
+  for (; i + (U - 1) * kDsThreads < in.z; i += U * kDsThreads) {
     u32x4 w[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) w[j] = r.v[i + j * kDsThreads];
+    float f[U * V];
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      float f[V];
-      unpack<DT>(w[j], f);
-      r.mask(i + j * kDsThreads, f);
-      add_values<DT, MODE>(f, V, c0, acc);
-    }
+    for (int j = 0; j < U; ++j) unpack<DT>(w[j], f + V * j);
+    add_values<MODE>(f, c0, acc);
   }
-  for (; i < z; i += kDsThreads) {
+  for (; i < in.z; i += kDsThreads) {
     float f[V];
     unpack<DT>(r.v[i], f);
-    r.mask(i, f);
-    add_values<DT, MODE>(f, V, c0, acc);
+    add_values<MODE>(f, c0, acc);
+  }
+  if (in.head || in.tail) {
+    float f[V];
+    const uint32_t e = in.head ? 0u : r.n - 1u;
+    unpack<DT>(r.v[e], f);
+    r.mask(e, f);
+    add_values<MODE>(f, c0, acc);
   }
   return acc;
 }
@@ -198,6 +214,9 @@ __device__ __forceinline__ double row_loss(const DistillArgs& g, uint32_t row, f
   return all * 0.693147180559945309417232121458176568;
 }
 
+// past the caches: they hold the rows that are read again
+__device__ __forceinline__ void store_vec(u32x4* p, u32x4 v) { __builtin_nontemporal_store(v, p); }
+
 // Gradient of vectors [a, z) of the row: w t (q - P). The teacher's entries are put
 // right after the vectors are written, each index by its first entry, from the
 // logit read before (grad may be x).
@@ -228,44 +247,55 @@ __device__ __forceinline__ void row_grad(const DistillArgs& g, uint32_t row, uin
   const bool same = ((uintptr_t)grow & 15u) == ((uintptr_t)xrow & 15u);
   u32x4* gv = reinterpret_cast<u32x4*>(grow - ((uintptr_t)grow & 15u));
   __syncthreads();   // every entry's logit has been read
-  auto one = [&](uint32_t i, const u32x4& w) {
-    float f[V];
+  auto values = [&](const u32x4& w, float* f) {
     unpack<DT>(w, f);
 #pragma unroll
     for (int k = 0; k < V; ++k) f[k] = qexp_row<MODE, true>(f[k], g.c0, c1) * scale;
-    if (same && i != 0 && i + 1 != r.n) {
-      gv[i] = pack<DT>(f);
-    } else {
+  };
+  auto put = [&](uint32_t i, const float* f) {   // element by element
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const uint32_t e = i * V + k;
-        if (e >= r.skip && e < r.skip + r.cols) store1<DT>(grow, e - r.skip, f[k]);
-      }
+    for (int k = 0; k < V; ++k) {
+      const uint32_t e = i * V + k;
+      if (e >= r.skip && e < r.skip + r.cols) store1<DT>(grow, e - r.skip, f[k]);
     }
   };
-  uint32_t i = a + threadIdx.x;
+  const Inner<DT> in(r, a, z);
+  float f[V] = {};
   if (scale == 0.0f) {
-    for (; i < z; i += kDsThreads) {
-      float f[V] = {};
-      if (same && i != 0 && i + 1 != r.n) {
-        gv[i] = pack<DT>(f);
-      } else {
+    for (uint32_t i = in.a + threadIdx.x; i < in.z; i += kDsThreads) {
+      if (same) gv[i] = u32x4{};
+      else put(i, f);
+    }
+    if (in.head) put(0, f);
+    if (in.tail) put(r.n - 1u, f);
+  } else {
+    // from the row's end on, which a pass before left in the nearest cache
+    const uint32_t count = in.z > in.a ? in.z - in.a : 0u;
+    uint32_t n = threadIdx.x;   // vectors from the end
+    if (same) {
+      for (; n + 3 * kDsThreads < count; n += 4 * kDsThreads) {
+        const uint32_t i = in.z - 1u - n;
+        u32x4 w[4];
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const uint32_t e = i * V + k;
-          if (e >= r.skip && e < r.skip + r.cols) store1<DT>(grow, e - r.skip, 0.0f);
+        for (int j = 0; j < 4; ++j) w[j] = r.v[i - j * kDsThreads];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          values(w[j], f);
+          store_vec(gv + (i - j * kDsThreads), pack<DT>(f));
         }
       }
     }
-  } else {
-    for (; i + 3 * kDsThreads < z; i += 4 * kDsThreads) {
-      u32x4 w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = r.v[i + j * kDsThreads];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) one(i + j * kDsThreads, w[j]);
+    for (; n < count; n += kDsThreads) {
+      const uint32_t i = in.z - 1u - n;
+      values(r.v[i], f);
+      if (same) gv[i] = pack<DT>(f);
+      else put(i, f);
     }
-    for (; i < z; i += kDsThreads) one(i, r.v[i]);
+    if (in.head || in.tail) {
+      const uint32_t e = in.head ? 0u : r.n - 1u;
+      values(r.v[e], f);
+      put(e, f);
+    }
   }
   if (!live) return;
   __syncthreads();   // the vectors are written
@@ -376,6 +406,12 @@ constexpr int64_t kDsFull = 512;
 static int64_t distill_chunks(int64_t rows, int64_t cols) {
   if (rows <= 0 || rows >= kDsFull) return 1;
   return std::max<int64_t>(1, std::min(kDsFull / rows, cols / 8192));
+}
+// Chunks of a row for the gradient alone: of 16384 elements also where the rows would
+// fill the GPU, as then the launch sweeps through memory from front to back (2048 x
+// 128256 bf16: 236 us with a workgroup per row, 190 us in chunks).
+static int64_t grad_chunks(int64_t rows, int64_t cols) {
+  return std::max(distill_chunks(rows, cols), std::max<int64_t>(1, cols / 16384));
 }
 static int64_t distill_ws_bytes(int64_t rows, int64_t cols) {
   const int64_t c = distill_chunks(rows, cols);
@@ -499,11 +535,12 @@ extern "C" quake_status quake_distill_grad(const void* x, const int32_t* idx, co
     return QUAKE_EINVAL;
   DistillArgs g{static_cast<const char*>(x), idx, static_cast<const char*>(y), weight, nullptr,
                 const_cast<float*>(stats), static_cast<char*>(grad), nullptr, ldx, ldi, ldy, ldg,
-                (uint32_t)cols, (uint32_t)topk, (uint32_t)distill_chunks(rows, cols),
+                (uint32_t)cols, (uint32_t)topk, (uint32_t)grad_chunks(rows, cols),
                 (int32_t)ydtype, c0, t};
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  for (int64_t r = 0; r < rows; r += kDsRows) {
-    const quake_status st = launch_distill(kGrad, dtype, mode, std::min(kDsRows, rows - r), s, g, r);
+  const int64_t most = std::max<int64_t>(1, kDsRows / g.chunks);
+  for (int64_t r = 0; r < rows; r += most) {
+    const quake_status st = launch_distill(kGrad, dtype, mode, std::min(most, rows - r), s, g, r);
     if (st != QUAKE_OK) return st;
   }
   return QUAKE_OK;

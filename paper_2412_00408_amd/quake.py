@@ -9,7 +9,6 @@ Build the library with ``python -m paper_2412_00408_amd.build``.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -218,8 +217,11 @@ def _span(t: torch.Tensor):
     """[first, last + 1) byte addresses a tensor view touches (empty: (0, 0))."""
     if t.numel() == 0:
         return 0, 0
-    last = sum((n - 1) * st for n, st in zip(t.shape, t.stride()))
-    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+    last = 1
+    for n, st in zip(t.shape, t.stride()):
+        last += (n - 1) * st
+    at = t.data_ptr()
+    return at, at + last * t.element_size()
 
 
 def _vt_row_stride(shape, strides) -> int:
@@ -337,53 +339,56 @@ def quake_softmax_causal(x, y=None, period=None, shift=0, mode=QUAKE_2, t=1.0, w
 # launches on the device of its first tensor, whichever is current.
 # ---------------------------------------------------------------------------
 _STRIDES = ctypes.c_int64 * 12
+_get_device = torch._C._cuda_getDevice
 
 
-def _on(device):
-    """The device to launch on, as a context (none where it is current already)."""
-    if device.index is None or device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+def _launch(name, device, *args):
+    """Call an entry point with `device` (an index) current."""
+    if device == _get_device():
+        rc = getattr(lib, name)(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(lib, name)(*args)
+    if rc != OK:
+        raise QuakeError(name, rc)
 
 
-def _operand(t, what, like=None, dtype=None, shape=None):
-    if not t.is_cuda:
-        raise ValueError("libquake takes device tensors")
-    if like is not None and t.device != like.device:
-        raise ValueError("%s must be on the device of the first tensor" % what)
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    if shape is not None and tuple(t.shape) != tuple(shape):
+def _operand(t, what, device, dtype=None, shape=None):
+    """t, on `device`, of the dtype (None: a format of the library) and shape."""
+    if t.get_device() != device or device < 0:
+        raise ValueError("libquake takes device tensors, %s on the first one's device" % what)
+    if t.dtype is not dtype and (dtype is not None or t.dtype not in DTYPES):
+        raise TypeError("%s must be %s, got %s" % (
+            what, "float32, float16 or bfloat16" if dtype is None else dtype, t.dtype))
+    if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
     return t
 
 
-def _per_row(t, what, x, n, dtype):
+def _per_row(t, what, device, n, dtype):
     """Device pointer of a contiguous vector of n values, or None."""
     if t is None:
         return None
-    _operand(t, what, x, dtype, (n,))
+    _operand(t, what, device, dtype, (n,))
     if n > 1 and t.stride(0) != 1:
         raise ValueError("%s must be contiguous" % what)
     return t.data_ptr()
 
 
-def _work(workspace, x):
+def _work(workspace, device):
     if workspace is None:
         return None, 0
-    _operand(workspace, "workspace", x)
-    if not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the first tensor's device")
+    return workspace.data_ptr(), workspace.nbytes
 
 
-def _apart(out, what, *others):
+def _apart(out, what, others):
+    """Refuses an output that shares bytes with one of others, (tensor, name) pairs."""
     o0, o1 = _span(out)
     for t, name in others:
-        if t is not None:
-            a0, a1 = _span(t)
-            if o0 < a1 and a0 < o1:
-                raise ValueError("%s must not overlap %s" % (what, name))
+        if t is not None and t.data_ptr() < o1 and o0 < _span(t)[1]:
+            raise ValueError("%s must not overlap %s" % (what, name))
 
 
 def _size(fn, *args):
@@ -414,38 +419,36 @@ def quake_attention_window(q, k, v, o=None, window=2**31 - 1, sinks=0, q_lens=No
     rows of o past q_lens keep what they held (a new o: undefined). t defaults to
     1/sqrt(dim). `workspace` (from attention_window_workspace) lets a call with few
     rows split its keys over more workgroups."""
+    dev, dt = q.get_device(), q.dtype
     for a, what in ((q, "q"), (k, "k"), (v, "v")):
-        _operand(a, what, q)
-        if a.dtype not in DTYPES:
-            raise TypeError("libquake takes float32, float16 or bfloat16 tensors, got %s" % a.dtype)
+        _operand(a, what, dev)
         if a.dim() != 4:
             raise ValueError("%s needs [batch, tokens, heads, dim]" % what)
-        if a.dtype != q.dtype:
-            raise TypeError("q, k and v must have the same dtype")
-    batch, sq, heads, dim = q.shape
-    if k.shape != v.shape or k.shape[0] != batch or k.shape[3] != dim:
+    if k.dtype is not dt or v.dtype is not dt:
+        raise TypeError("q, k and v must have the same dtype")
+    batch, sq, heads, dim = shape = q.shape
+    kvshape = k.shape
+    skv, kv_heads = kvshape[1], kvshape[2]
+    if v.shape != kvshape or kvshape[0] != batch or kvshape[3] != dim:
         raise ValueError("k and v must be [batch, skv, kv_heads, dim] with q's batch and dim")
-    skv, kv_heads = k.shape[1], k.shape[2]
     if kv_heads == 0 or heads % kv_heads:
         raise ValueError("heads must be a multiple of kv_heads")
     if o is None:
-        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        o = torch.empty(shape, dtype=dt, device=q.device)
     else:
-        _operand(o, "o", q, q.dtype, q.shape)
-        _apart(o, "o", (q, "q"), (k, "k"), (v, "v"), (q_lens, "q_lens"), (kv_lens, "kv_lens"))
-    for a, what in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
-        if a.stride(3) != 1:
-            raise ValueError("%s must have a contiguous last dimension" % what)
-    st = _STRIDES(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3])
-    ql = _per_row(q_lens, "q_lens", q, batch, torch.int32)
-    kl = _per_row(kv_lens, "kv_lens", q, batch, torch.int32)
-    ws, nbytes = _work(workspace, q)
-    t = 1.0 / dim ** 0.5 if t is None else t
-    with _on(q.device):
-        _raise("quake_attention_window", lib.quake_attention_window(
-            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), ql, kl, batch, sq, skv, heads,
-            kv_heads, dim, st, min(window, 2**31 - 1), sinks, DTYPES[q.dtype], MODES[mode], t, ws,
-            nbytes, _stream(q, stream)))
+        _operand(o, "o", dev, dt, shape)
+        _apart(o, "o", ((q, "q"), (k, "k"), (v, "v"), (q_lens, "q_lens"), (kv_lens, "kv_lens")))
+    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), o.stride()
+    if not qs[3] == ks[3] == vs[3] == os_[3] == 1:
+        raise ValueError("q, k, v and o must have a contiguous last dimension")
+    ql = _per_row(q_lens, "q_lens", dev, batch, torch.int32)
+    kl = _per_row(kv_lens, "kv_lens", dev, batch, torch.int32)
+    ws, nbytes = _work(workspace, dev)
+    _launch("quake_attention_window", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+            ql, kl, batch, sq, skv, heads, kv_heads, dim,
+            _STRIDES(*qs[:3], *ks[:3], *vs[:3], *os_[:3]), min(window, 2**31 - 1), sinks,
+            DTYPES[dt], MODES[mode], 1.0 / dim ** 0.5 if t is None else t, ws, nbytes,
+            _stream(q, stream))
     return o
 
 
@@ -455,19 +458,20 @@ def sample_workspace(x):
     return _new_workspace(_size("quake_sample_workspace_size", x.shape[0], x.shape[1]), x.device)
 
 
-def _matrix(x, what):
-    _operand(x, what)
-    if x.dtype not in DTYPES:
-        raise TypeError("libquake takes float32, float16 or bfloat16 tensors, got %s" % x.dtype)
+def _matrix(x, what, device):
+    """Row stride of a matrix of rows on `device`."""
+    _operand(x, what, device)
     if x.dim() != 2:
         raise ValueError("%s must be [rows, cols]" % what)
     return _row_stride(x, what)
 
 
 def _row_stride(x, what):
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    rows, cols = x.shape
+    ld, one = x.stride()
+    if one != 1 and cols > 1:
         raise ValueError("%s must have a contiguous last dimension" % what)
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return ld if rows > 1 else cols
 
 
 def quake_sample(x, u, token=None, prob=None, temperature=None, top_k=None, top_p=None,
@@ -478,31 +482,32 @@ def quake_sample(x, u, token=None, prob=None, temperature=None, top_k=None, top_
     temperature, top_p, min_p: float32 [rows], top_k: int32 [rows], or None (1, and
     no filter); temperature 0 takes the largest logit. `workspace` (from
     sample_workspace) lets several workgroups read a row."""
-    ldx = _matrix(x, "x")
+    dev = x.get_device()
+    ldx = _matrix(x, "x", dev)
     rows, cols = x.shape
     if u is None:
         raise ValueError("u must be float32 [rows]")
-    vecs = [_per_row(a, what, x, rows, dt) for a, what, dt in (
-        (u, "u", torch.float32), (temperature, "temperature", torch.float32),
-        (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
-        (min_p, "min_p", torch.float32))]
-    inputs = ((x, "x"), (u, "u"), (temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"),
-              (min_p, "min_p"))
+    f32, i32 = torch.float32, torch.int32
+    up = _per_row(u, "u", dev, rows, f32)
+    tp = _per_row(temperature, "temperature", dev, rows, f32)
+    kp = _per_row(top_k, "top_k", dev, rows, i32)
+    pp = _per_row(top_p, "top_p", dev, rows, f32)
+    mp = _per_row(min_p, "min_p", dev, rows, f32)
     if token is None:
-        token = torch.empty(rows, dtype=torch.int32, device=x.device)
+        token = torch.empty(rows, dtype=i32, device=x.device)
     else:
-        _per_row(token, "token", x, rows, torch.int32)
-        _apart(token, "token", *inputs)
+        _per_row(token, "token", dev, rows, i32)
+        _apart(token, "token", ((x, "x"), (u, "u"), (temperature, "temperature"), (top_k, "top_k"),
+                                (top_p, "top_p"), (min_p, "min_p")))
     if prob is None:
-        prob = torch.empty(rows, dtype=torch.float32, device=x.device)
+        prob = torch.empty(rows, dtype=f32, device=x.device)
     else:
-        _per_row(prob, "prob", x, rows, torch.float32)
-        _apart(prob, "prob", (token, "token"), *inputs)
-    ws, nbytes = _work(workspace, x)
-    with _on(x.device):
-        _raise("quake_sample", lib.quake_sample(
-            x.data_ptr(), vecs[0], token.data_ptr(), prob.data_ptr(), rows, cols, ldx, *vecs[1:],
-            DTYPES[x.dtype], MODES[mode], ws, nbytes, _stream(x, stream)))
+        _per_row(prob, "prob", dev, rows, f32)
+        _apart(prob, "prob", ((token, "token"), (x, "x"), (u, "u"), (temperature, "temperature"),
+                              (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p")))
+    ws, nbytes = _work(workspace, dev)
+    _launch("quake_sample", dev, x.data_ptr(), up, token.data_ptr(), prob.data_ptr(), rows, cols,
+            ldx, tp, kp, pp, mp, DTYPES[x.dtype], MODES[mode], ws, nbytes, _stream(x, stream))
     return token, prob
 
 
@@ -512,27 +517,27 @@ def distill_workspace(x):
     return _new_workspace(_size("quake_distill_workspace_size", x.shape[0], x.shape[1]), x.device)
 
 
-def _distill_args(x, idx, y, weight):
-    ldx = _matrix(x, "x")
+def _distill_args(x, idx, y, weight, dev):
+    ldx = _matrix(x, "x", dev)
     rows, cols = x.shape
-    topk = idx.shape[1] if idx.dim() == 2 else 0
-    _operand(idx, "idx", x, torch.int32, (rows, topk))
-    _operand(y, "y", x, None, (rows, topk))
-    if y.dtype not in DTYPES:
-        raise TypeError("libquake takes float32, float16 or bfloat16 tensors, got %s" % y.dtype)
-    return (rows, cols, topk, ldx, _row_stride(idx, "idx"), _row_stride(y, "y"),
-            _per_row(weight, "weight", x, rows, torch.float32))
+    shape = idx.shape
+    if len(shape) != 2 or shape[0] != rows:
+        raise ValueError("idx and y must be [rows, topk]")
+    _operand(idx, "idx", dev, torch.int32)
+    _operand(y, "y", dev, None, shape)
+    return (rows, cols, shape[1], ldx, _row_stride(idx, "idx"), _row_stride(y, "y"),
+            _per_row(weight, "weight", dev, rows, torch.float32))
 
 
-def _distill_grad_out(x, grad, *others):
+def _distill_grad_out(x, grad, dev, others):
     """grad's row stride; x itself, or apart from every operand."""
-    _operand(grad, "grad", x, x.dtype, x.shape)
+    _operand(grad, "grad", dev, x.dtype, x.shape)
     ldg = _row_stride(grad, "grad")
-    if grad.data_ptr() != x.data_ptr() or (x.shape[0] > 1 and grad.stride(0) != x.stride(0)):
-        _apart(grad, "grad", (x, "x"))
     if grad.shape[0] > 1 and ldg < grad.shape[1]:
         raise ValueError("grad's rows must not overlap")
-    _apart(grad, "grad", *others)
+    if grad.data_ptr() != x.data_ptr() or (x.shape[0] > 1 and grad.stride(0) != x.stride(0)):
+        _apart(grad, "grad", ((x, "x"),))
+    _apart(grad, "grad", others)
     return ldg
 
 
@@ -544,43 +549,41 @@ def quake_distill(x, idx, y, weight=None, grad=None, mode=QUAKE_2, t=1.0, worksp
     d(sum weight * loss)/dx, of x's dtype, where `grad` is True or a tensor to
     write it to (x itself: in place), else None. `workspace` (from
     distill_workspace) cuts few rows into chunks."""
-    rows, cols, topk, ldx, ldi, ldy, w = _distill_args(x, idx, y, weight)
-    ws, nbytes = _work(workspace, x)
+    dev = x.get_device()
+    rows, cols, topk, ldx, ldi, ldy, w = _distill_args(x, idx, y, weight, dev)
+    ws, nbytes = _work(workspace, dev)
     loss = torch.empty(rows, dtype=torch.float32, device=x.device)
     stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
     ldg, gp = cols, None
-    if grad is True:
-        grad = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    elif grad is False:
+    if grad is False:
         grad = None
+    elif grad is True:
+        grad = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
     elif grad is not None:
-        ldg = _distill_grad_out(x, grad, (idx, "idx"), (y, "y"), (weight, "weight"))
+        ldg = _distill_grad_out(x, grad, dev, ((idx, "idx"), (y, "y"), (weight, "weight")))
     if grad is not None:
         gp = grad.data_ptr()
-    with _on(x.device):
-        _raise("quake_distill", lib.quake_distill(
-            x.data_ptr(), idx.data_ptr(), y.data_ptr(), w, loss.data_ptr(), stats.data_ptr(), gp,
-            rows, cols, topk, ldx, ldi, ldy, ldg, DTYPES[x.dtype], DTYPES[y.dtype], MODES[mode], t,
-            ws, nbytes, _stream(x, stream)))
+    _launch("quake_distill", dev, x.data_ptr(), idx.data_ptr(), y.data_ptr(), w, loss.data_ptr(),
+            stats.data_ptr(), gp, rows, cols, topk, ldx, ldi, ldy, ldg, DTYPES[x.dtype],
+            DTYPES[y.dtype], MODES[mode], t, ws, nbytes, _stream(x, stream))
     return loss, stats, grad
 
 
 def quake_distill_grad(x, idx, y, stats, weight=None, grad=None, mode=QUAKE_2, t=1.0, stream=None):
     """weight * d loss / dx of quake_distill(x, idx, y) from the stats it returned
     (same mode and t), into `grad` (default a new tensor; x itself: in place)."""
-    rows, cols, topk, ldx, ldi, ldy, w = _distill_args(x, idx, y, weight)
-    _operand(stats, "stats", x, torch.float32, (rows, 2))
+    dev = x.get_device()
+    rows, cols, topk, ldx, ldi, ldy, w = _distill_args(x, idx, y, weight, dev)
+    _operand(stats, "stats", dev, torch.float32, (rows, 2))
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
     ldg = cols
     if grad is None:
         grad = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
     else:
-        ldg = _distill_grad_out(x, grad, (idx, "idx"), (y, "y"), (weight, "weight"),
-                                (stats, "stats"))
-    with _on(x.device):
-        _raise("quake_distill_grad", lib.quake_distill_grad(
-            x.data_ptr(), idx.data_ptr(), y.data_ptr(), stats.data_ptr(), w, grad.data_ptr(), rows,
-            cols, topk, ldx, ldi, ldy, ldg, DTYPES[x.dtype], DTYPES[y.dtype], MODES[mode], t,
-            _stream(x, stream)))
+        ldg = _distill_grad_out(x, grad, dev, ((idx, "idx"), (y, "y"), (weight, "weight"),
+                                               (stats, "stats")))
+    _launch("quake_distill_grad", dev, x.data_ptr(), idx.data_ptr(), y.data_ptr(),
+            stats.data_ptr(), w, grad.data_ptr(), rows, cols, topk, ldx, ldi, ldy, ldg,
+            DTYPES[x.dtype], DTYPES[y.dtype], MODES[mode], t, _stream(x, stream))
     return grad
