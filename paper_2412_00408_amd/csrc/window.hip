@@ -366,6 +366,7 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
           reinterpret_cast<const float*>(s_buf + w * kWave)[(d0 + i) * 32 + fr], e[w]);
   }
   if (g.nsplit > 1) {
+    if (r0 + fr >= rows) return;
     float* w = g.ws + (int64_t)blockIdx.x * (64 + 32 * D);
     if (wave == 0 && h == 0) {
       w[fr] = m;
@@ -583,6 +584,7 @@ __global__ __launch_bounds__(64 * kWinWaves, 2) void window_many_kernel(WindowAr
   if (g.nsplit > 1) {
     if (w0 >= rows) return;
     const int64_t slot32 = ((int64_t)bh * g.tiles + kWinWaves * tile + wave) * g.nsplit + split;
+    if (w0 + fr >= rows) return;
     float* w = g.ws + slot32 * (64 + 32 * D);
     if (h == 0) {
       w[fr] = acc.m;
@@ -622,43 +624,72 @@ __global__ __launch_bounds__(64 * kWinWaves, 2) void window_many_kernel(WindowAr
   }
 }
 
-// Joins the splits of a tile: thread t takes D / 8 dims of row t / 8.
-template <int DT, int D>
+// Joins a row's splits, a lane for every four dims: D / 4 lanes, which take the splits
+// one after the other, or (WIDE) the whole workgroup, whose 1024 / D such teams take
+// every so many-th. Several loads are in flight; the order is fixed.
+template <int DT, int D, bool WIDE>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs g) {
-  const int tile = blockIdx.x % (uint32_t)g.tiles;
-  const int hk = (blockIdx.x / (uint32_t)g.tiles) % (uint32_t)g.kv_heads;
-  const int b = blockIdx.x / (uint32_t)g.tiles / (uint32_t)g.kv_heads;
-  const int32_t rows = seq_len(g.q_lens, b, g.sq) * g.group;
-  const int fr = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * (D / 8);
+  constexpr int C = D / 4, SL = WIDE ? 256 / C : 1, U = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t id = WIDE ? blockIdx.x : blockIdx.x * (256u / C) + threadIdx.x / C;   // of all rows
+  const uint32_t item = id >> 5;
+  const int fr = id & 31u, tile = item % (uint32_t)g.tiles;
+  const int hk = (item / (uint32_t)g.tiles) % (uint32_t)g.kv_heads;
+  const int b = item / (uint32_t)g.tiles / (uint32_t)g.kv_heads;
   const int32_t row = 32 * tile + fr;
-  if (row >= rows) return;
-  const int64_t slot = 64 + 32 * D;
-  const float* w = g.ws + (int64_t)blockIdx.x * g.nsplit * slot;
-  float m = kNoMax;
-  for (int s = 0; s < g.nsplit; ++s) m = fmaxf(m, w[s * slot + fr]);
-  float sum = 0.0f, v[D / 8] = {};
-  for (int s = 0; s < g.nsplit; ++s) {
-    const int32_t e = down_shift(w[s * slot + fr], m);
-    sum += __builtin_amdgcn_ldexpf(w[s * slot + 32 + fr], e);
+  if (row >= seq_len(g.q_lens, b, g.sq) * g.group) return;
+  constexpr int64_t slot = 64 + 32 * D;
+  const float* w = g.ws + (int64_t)item * g.nsplit * slot;
+  const int c = lane % C;
+  float m = kNoMax, sum = 0.0f;
+  float4 v{0.0f, 0.0f, 0.0f, 0.0f};
+  auto add = [&](float om, float os, float4 ov) {
+    const float top = fmaxf(m, om);
+    const int32_t e = down_shift(m, top), oe = down_shift(om, top);
+    auto two = [&](float a, float o) {
+      return __builtin_amdgcn_ldexpf(a, e) + __builtin_amdgcn_ldexpf(o, oe);
+    };
+    sum = two(sum, os);
+    v = float4{two(v.x, ov.x), two(v.y, ov.y), two(v.z, ov.z), two(v.w, ov.w)};
+    m = top;
+  };
+  for (int s0 = WIDE ? threadIdx.x / C : 0; s0 < g.nsplit; s0 += U * SL) {
+    float om[U], os[U];
+    float4 ov[U];
 #pragma unroll
-    for (int i = 0; i < D / 8; i += 4) {
-      const float4 x = *reinterpret_cast<const float4*>(w + s * slot + 64 + fr * D + d0 + i);
-      v[i] += __builtin_amdgcn_ldexpf(x.x, e);
-      v[i + 1] += __builtin_amdgcn_ldexpf(x.y, e);
-      v[i + 2] += __builtin_amdgcn_ldexpf(x.z, e);
-      v[i + 3] += __builtin_amdgcn_ldexpf(x.w, e);
+    for (int j = 0; j < U; ++j) {   // past the last split: that one again, not added
+      const float* p = w + (int64_t)min(s0 + j * SL, g.nsplit - 1) * slot;
+      om[j] = p[fr];
+      os[j] = p[32 + fr];
+      ov[j] = *reinterpret_cast<const float4*>(p + 64 + fr * D + 4 * c);
     }
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (s0 + j * SL < g.nsplit) add(om[j], os[j], ov[j]);
+  }
+  if constexpr (WIDE) {
+    constexpr int W = 4;
+#pragma unroll
+    for (int o = C; o < 64; o <<= 1)
+      add(__shfl_xor(m, o, 64), __shfl_xor(sum, o, 64),
+          float4{__shfl_xor(v.x, o, 64), __shfl_xor(v.y, o, 64), __shfl_xor(v.z, o, 64),
+                 __shfl_xor(v.w, o, 64)});
+    __shared__ float s_m[W], s_sum[W];
+    __shared__ float4 s_v[W][C];
+    if (lane < C) s_v[wave][c] = v;
+    if (lane == 0) {
+      s_m[wave] = m;
+      s_sum[wave] = sum;
+    }
+    __syncthreads();
+    if (wave > 0 || lane >= C) return;
+#pragma unroll
+    for (int o = 1; o < W; ++o) add(s_m[o], s_sum[o], s_v[o][c]);
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  uint16_t* orow = g.o + b * g.ob + (row / g.group) * g.os +
-                   (hk * g.group + row % g.group) * g.oh + d0;
-#pragma unroll
-  for (int i = 0; i < D / 8; i += 8) {
-    u32x4 x;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = wpack<DT>(v[i + 2 * j] * inv, v[i + 2 * j + 1] * inv);
-    *reinterpret_cast<u32x4*>(orow + i) = x;
-  }
+  uint16_t* orow = g.o + b * g.ob + (row / g.group) * g.os + (hk * g.group + row % g.group) * g.oh;
+  *reinterpret_cast<u32x2*>(orow + 4 * c) =
+      u32x2{wpack<DT>(v.x * inv, v.y * inv), wpack<DT>(v.z * inv, v.w * inv)};
 }
 
 // ---------------------------------------------------------------------------
@@ -671,9 +702,11 @@ struct WindowPlan {
 };
 
 // Splits: few tiles leave compute units idle while each walks a long window, so a
-// tile's keys go to as many workgroups as bring the launch to kWinTarget, with at
-// least 256 keys for each.
-constexpr int64_t kWinTarget = 512;
+// tile's keys go to as many workgroups as bring the launch to kWinTarget (one per
+// compute unit), with at least kSplitKeys keys for each. Below kSplitFrom keys the
+// second launch costs more than it saves.
+constexpr int64_t kWinTarget = 256, kSplitKeys = 128, kSplitFrom = 512;
+constexpr int64_t kJoinFew = 8;     // splits up to which D / 4 lanes join a row
 constexpr int64_t kManyRows = 96;   // rows from which on 128 share a workgroup
 
 static WindowPlan window_plan(int64_t batch, int64_t sq, int64_t skv, int64_t group,
@@ -686,7 +719,7 @@ static WindowPlan window_plan(int64_t batch, int64_t sq, int64_t skv, int64_t gr
   const int64_t items = batch * kv_heads * ((rows + wide - 1) / wide);
   const int64_t queries = (wide - 1 + group) / group;   // most positions a tile covers, less one
   const int64_t keys = std::min(skv, std::min(window, skv) + std::min(sinks, skv) + queries);
-  const int64_t most = (keys + 255) / 256;
+  const int64_t most = keys < kSplitFrom ? 1 : keys / kSplitKeys;
   p.nsplit = items == 0 ? 1 : std::max<int64_t>(1, std::min(most, kWinTarget / items));
   return p;
 }
@@ -715,9 +748,12 @@ static void launch_window(bool many, int64_t heads, hipStream_t s, const WindowA
     hipLaunchKernelGGL((window_many_kernel<DT, MODE, D>), grid, dim3(64 * kWinWaves), 0, s, g);
   else
     hipLaunchKernelGGL((window_few_kernel<DT, MODE, D>), grid, dim3(64 * kWinWaves), 0, s, g);
-  if (g.nsplit > 1)
-    hipLaunchKernelGGL((window_join_kernel<DT, D>), dim3((uint32_t)(heads * g.tiles)), dim3(256), 0,
-                       s, g);
+  if (g.nsplit > kJoinFew)
+    hipLaunchKernelGGL((window_join_kernel<DT, D, true>), dim3((uint32_t)(heads * g.tiles * 32)),
+                       dim3(256), 0, s, g);
+  else if (g.nsplit > 1)
+    hipLaunchKernelGGL((window_join_kernel<DT, D, false>), dim3((uint32_t)(heads * g.tiles * D / 32)),
+                       dim3(256), 0, s, g);
 }
 template <int DT, int D>
 static void launch_window(int mode, bool many, int64_t heads, hipStream_t s, const WindowArgs& g) {
