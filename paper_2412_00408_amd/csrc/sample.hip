@@ -366,41 +366,44 @@ __device__ __forceinline__ uint32_t seg_of(uint32_t n, uint32_t vec, uint32_t ns
   return (uint32_t)(((uint64_t)(vec + 1u) * nseg - 1u) / n);
 }
 
-// f(vector index, elements) for vectors [a, z) by NW waves; elements outside the row
-// and vectors from z on -inf. Every lane takes part in every call.
+// f(vector index, elements) for vectors [a, z) by NW waves, each by one lane; elements
+// outside the row are -inf (the row's first and last vector are masked, no others).
 template <int NW, int U, int DT, typename F>
 __device__ __forceinline__ void each_vector(const RowVecs<DT>& r, uint32_t a, uint32_t z, F f) {
   constexpr uint32_t V = kV<DT>, T = 64 * NW;
-  const uint32_t t = threadIdx.x & (T - 1u);
-  uint32_t base = a;
-  for (; base + U * T <= z; base += U * T) {
+  const uint32_t t = threadIdx.x & (T - 1u), in = min(z, r.n - 1u);
+  uint32_t i = max(a, 1u) + t;
+  for (; i + (U - 1) * T < in; i += U * T) {
     u32x4 w[U];
 #pragma unroll
-    for (uint32_t j = 0; j < U; ++j) w[j] = r.v[base + t + T * j];
+    for (uint32_t j = 0; j < U; ++j) w[j] = r.v[i + T * j];
 #pragma unroll
     for (uint32_t j = 0; j < U; ++j) {
       float v[V];
       unpack<DT>(w[j], v);
-      r.mask(base + t + T * j, v);
-      f(base + t + T * j, v);
+      f(i + T * j, v);
     }
   }
-  if (base >= z) return;
-  u32x4 w[U];
+  if (i < in) {
+    u32x4 w[U];
 #pragma unroll
-  for (uint32_t j = 0; j < U; ++j) w[j] = r.v[min(base + t + T * j, z - 1u)];
+    for (uint32_t j = 0; j < U; ++j) w[j] = r.v[min(i + T * j, in - 1u)];
 #pragma unroll
-  for (uint32_t j = 0; j < U; ++j) {
-    if (base + T * j < z) {
-      float v[V];
-      unpack<DT>(w[j], v);
-      r.mask(base + t + T * j, v);
-      if (base + t + T * j >= z) {
-#pragma unroll
-        for (uint32_t k = 0; k < V; ++k) v[k] = -INFINITY;
+    for (uint32_t j = 0; j < U; ++j) {
+      if (i + T * j < in) {
+        float v[V];
+        unpack<DT>(w[j], v);
+        f(i + T * j, v);
       }
-      f(base + t + T * j, v);
     }
+  }
+  const bool head = a == 0 && z > 0 && t == 0, tail = a < z && z == r.n && r.n > 1u && t == T - 1u;
+  if (head || tail) {
+    const uint32_t e = head ? 0u : r.n - 1u;
+    float v[V];
+    unpack<DT>(r.v[e], v);
+    r.mask(e, v);
+    f(e, v);
   }
 }
 
@@ -440,21 +443,6 @@ __device__ __forceinline__ float kth_bound(const float (&v)[N], uint32_t k, Samp
     } else {
       hi = mid;
     }
-  }
-  return lo;
-}
-
-// A value that k of the wave's 64 reach (most: the largest): as kth_bound, by ballots
-// alone. -inf where fewer are above it.
-__device__ __forceinline__ float wave_kth(float v, float most, uint32_t k) {
-  float lo = -wave_max(v > -INFINITY ? -v : -INFINITY), hi = most;
-  if (!(lo <= hi) || (uint32_t)__popcll(__ballot(v >= lo)) < k) return -INFINITY;
-  for (int i = 0; i < 12; ++i) {
-    const float mid = 0.5f * lo + 0.5f * hi;
-    const uint32_t c = (uint32_t)__popcll(__ballot(v >= mid));
-    if (c >= k) lo = mid;
-    else hi = mid;
-    if (c == k) break;
   }
   return lo;
 }
@@ -802,7 +790,7 @@ template <int DT, int MODE>
 __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void sample_row_kernel(SampleArgs g, uint32_t row0) {
   __shared__ SampleShared sh;
-  constexpr int U = 4;
+  constexpr int U = kV<DT> == 4 ? 4 : 2;   // vectors in flight: no more registers than there are
   const uint32_t row = row0 + blockIdx.x;
   const RowVecs<DT> v(g.x + (int64_t)row * g.ldx * kEsz<DT>, g.cols);
   RowSampler<DT, MODE> r;
@@ -810,7 +798,7 @@ void sample_row_kernel(SampleArgs g, uint32_t row0) {
   r.cols = g.cols;
   r.p = row_params<MODE>(g, row);
   float top[1] = {-INFINITY};
-  each_vector<kRowWaves, U>(v, 0, v.n, [&](uint32_t, const float* f) {
+  each_vector<kRowWaves, 8>(v, 0, v.n, [&](uint32_t, const float* f) {
 #pragma unroll
     for (int k = 0; k < kV<DT>; ++k) top[0] = fmaxf(top[0], f[k]);
   });
@@ -827,7 +815,7 @@ void sample_row_kernel(SampleArgs g, uint32_t row0) {
   if (kind == kTopK) {
     const float above = kth_bound<kRowWaves>(top, r.p.k, sh) - slack<MODE>(r.p);
     __syncthreads();
-    each_vector<kRowWaves, U>(v, 0, v.n, [&](uint32_t i, const float* f) {
+    each_vector<kRowWaves, 8>(v, 0, v.n, [&](uint32_t i, const float* f) {
       add_above<DT>(f, i * kV<DT> - v.skip, above, sh);
     });
     __syncthreads();
@@ -860,20 +848,22 @@ void sample_row_kernel(SampleArgs g, uint32_t row0) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: the passes by several workgroups per row (one would be bound by one
-// compute unit's loads and arithmetic), a launch each, the rest by one.
-//   scan    each part's max; top-k rows: the part's candidates, above the least of the
-//           values that k / 4 of each wave's lanes' maxima reach
+// Few long rows without a top-k: the passes by several workgroups per row (one would
+// be bound by one compute unit's loads and arithmetic), a launch each, the rest by one.
+//   scan    each part's max; greedy rows: its first word
 //   mass    top-p rows: the bins; unranked rows: the parts' kept masses
 //   cut     top-p rows: the cut bin's candidates and the parts' kept masses
 //   finish  the token
+// (With a top-k one workgroup a row was faster at every size: two passes of a compare
+// a word and one launch, 22 against 26 us for 64 x 128256 binary32.)
 // ---------------------------------------------------------------------------
 constexpr int kPartThreads = 256, kPartWaves = 4;
 constexpr uint32_t kWsCap = 16384;       // candidates of a row in the workspace
 
 // Workspace of a row: bins, candidates (each part has its share of the places), the
-// parts' masses, masses kept, maxima and counts of candidates. Every word that a
-// launch reads, an earlier one of the same call has written.
+// parts' masses, masses kept, maxima and counts of candidates (greedy rows: the first
+// word of the part's max). Every word that a launch reads, an earlier one of the same
+// call has written.
 struct SampleWs {
   char* base;
   int64_t stride;
@@ -922,10 +912,15 @@ __device__ __forceinline__ uint32_t fetch_list(const SampleWs& ws, uint32_t row,
   return (uint32_t)all;
 }
 
-template <int DT, int MODE>
+// a greedy row of a call without a top-k
+__device__ __forceinline__ bool is_greedy(const SampleArgs& g, uint32_t row) {
+  return g.temperature != nullptr && !(g.temperature[row] > 0.0f);
+}
+
+template <int DT>
 __global__ __launch_bounds__(kPartThreads) void sample_scan_kernel(SampleArgs g, SampleWs ws) {
-  __shared__ ListShared<1024> sh;
-  __shared__ float s_top[kPartWaves], s_bound[kPartWaves];
+  __shared__ float s_top[kPartWaves];
+  __shared__ uint32_t s_first;
   constexpr int V = kV<DT>, N = 8192 / (V * kPartThreads);
   const uint32_t row = blockIdx.x / ws.parts, part = blockIdx.x % ws.parts;
   const RowVecs<DT> v(g.x + (int64_t)row * g.ldx * kEsz<DT>, g.cols);
@@ -933,47 +928,36 @@ __global__ __launch_bounds__(kPartThreads) void sample_scan_kernel(SampleArgs g,
   u32x4 w[N];   // the part, in registers
 #pragma unroll
   for (int j = 0; j < N; ++j) w[j] = v.v[min(a + threadIdx.x + j * kPartThreads, z - 1u)];
-  const RowParams p = row_params<MODE>(g, row);
   if (part == 0)
     for (uint32_t i = threadIdx.x; i < kWeightBins; i += kPartThreads) ws.hist(row)[i] = 0;
+  if (threadIdx.x == 0) s_first = 0xFFFFFFFFu;
   float top = -INFINITY;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const uint32_t i = a + threadIdx.x + j * kPartThreads;
     float f[V];
     unpack<DT>(w[j], f);
-    v.mask(min(i, z - 1u), f);
-    if (i < z) {   // no word twice
+    v.mask(min(a + threadIdx.x + j * kPartThreads, z - 1u), f);
 #pragma unroll
-      for (int k = 0; k < V; ++k) top = fmaxf(top, f[k]);
-    }
+    for (int k = 0; k < V; ++k) top = fmaxf(top, f[k]);
   }
-  const bool top_k = row_kind(p, g.cols) == kTopK;
-  const float most = wave_max(top);
-  float bound = -INFINITY;
-  if (top_k) bound = wave_kth(top, most, (p.k + kPartWaves - 1u) / kPartWaves);
-  if ((threadIdx.x & 63u) == 0) {
-    s_top[threadIdx.x >> 6] = most;
-    s_bound[threadIdx.x >> 6] = bound;
-  }
-  if (threadIdx.x == 0) sh.count = 0;
+  top = wave_max(top);
+  if ((threadIdx.x & 63u) == 0) s_top[threadIdx.x >> 6] = top;
   __syncthreads();
-  if (threadIdx.x == 0)
-    ws.maxima(row)[part] = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-  if (!top_k) return;
-  const float above = fminf(fminf(s_bound[0], s_bound[1]), fminf(s_bound[2], s_bound[3])) -
-                      slack<MODE>(p);
+  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  if (threadIdx.x == 0) ws.maxima(row)[part] = top;
+  if (!is_greedy(g, row)) return;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const uint32_t i = a + threadIdx.x + j * kPartThreads;
-    if (i < z) {
-      float f[V];
-      unpack<DT>(w[j], f);
-      v.mask(i, f);
-      add_above<DT>(f, i * V - v.skip, above, sh);
-    }
+    const uint32_t i = min(a + threadIdx.x + j * kPartThreads, z - 1u);
+    float f[V];
+    unpack<DT>(w[j], f);
+    v.mask(i, f);
+#pragma unroll
+    for (int k = V - 1; k >= 0; --k)
+      if (f[k] == top && f[k] > -INFINITY) atomicMin(&s_first, i * V + k - v.skip);
   }
-  flush_list(ws, row, part, sh);
+  __syncthreads();
+  if (threadIdx.x == 0) ws.count(row)[part] = s_first;
 }
 
 template <int NW>
@@ -988,13 +972,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_mass_kernel(SampleArgs g,
   __shared__ SampleShared sh;
   const uint32_t row = blockIdx.x / ws.parts, part = blockIdx.x % ws.parts;
   const RowParams p = row_params<MODE>(g, row);
-  if (row_kind(p, g.cols) == kTopK) return;
   const float m = row_max<kPartWaves>(ws, row, sh);
   const RowKind kind = row_kind(p, g.cols, m);
-  if (kind != kTopP && kind != kPlain) return;
+  if (is_greedy(g, row) || (kind != kTopP && kind != kPlain)) return;
   const RowVecs<DT> v(g.x + (int64_t)row * g.ldx * kEsz<DT>, g.cols);
   const uint32_t a = seg_begin(v.n, part, ws.parts), z = seg_begin(v.n, part + 1, ws.parts);
-  constexpr int U = 4;
+  constexpr int U = kV<DT> == 4 ? 4 : 2;
   uint64_t mass;
   if (kind == kPlain) {
     mass = plain_mass<DT, MODE, kPartWaves, U>(v, a, z, m, p, least_kept(p));
@@ -1027,15 +1010,14 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs g, 
   __shared__ SampleShared sh;
   const uint32_t row = blockIdx.x / ws.parts, part = blockIdx.x % ws.parts;
   const RowParams p = row_params<MODE>(g, row);
-  if (row_kind(p, g.cols) != kTopP) return;
   const float m = row_max<kPartWaves>(ws, row, sh);
-  if (row_kind(p, g.cols, m) != kTopP) return;
+  if (is_greedy(g, row) || row_kind(p, g.cols, m) != kTopP) return;
   if (threadIdx.x == 0) sh.count = 0;
   const Cut c = row_cut<kPartWaves>(ws, row, ws.mass(row), p, sh);
   const RowVecs<DT> v(g.x + (int64_t)row * g.ldx * kEsz<DT>, g.cols);
   const uint32_t a = seg_begin(v.n, part, ws.parts), z = seg_begin(v.n, part + 1, ws.parts);
   const uint64_t mass = block_sum64<kPartWaves>(
-      cut_mass<DT, MODE, kPartWaves, 4>(v, a, z, m, p, c, sh), sh);
+      cut_mass<DT, MODE, kPartWaves, kV<DT> == 4 ? 4 : 2>(v, a, z, m, p, c, sh), sh);
   if (threadIdx.x == 0) ws.kept(row)[part] = mass;
   flush_list(ws, row, part, sh);
 }
@@ -1056,11 +1038,18 @@ void sample_finish_kernel(SampleArgs g, SampleWs ws) {
     write_none(g, row);
     return;
   }
-  const uint32_t n = kind == kTopK || kind == kTopP ? fetch_list(ws, row, sh) : 0u;
-  if (kind == kTopK && n <= kCap) {
-    finish_top_k(g, row, weigh_list<MODE>(n, m, r.p, sh), r.p, sh);
+  if (is_greedy(g, row)) {   // the first word of the row's max
+    uint32_t first = 0xFFFFFFFFu;
+    if (threadIdx.x < ws.parts && ws.maxima(row)[threadIdx.x] == m) first = ws.count(row)[threadIdx.x];
+    if (threadIdx.x == 0) sh.found = 0xFFFFFFFFu;
+    __syncthreads();
+    if (first != 0xFFFFFFFFu) atomicMin(&sh.found, first);
+    __syncthreads();
+    if (threadIdx.x == 0) write_row(g, row, sh.found, 1u, 1u);
     return;
-  } else if (kind == kTopP && n <= kCap) {
+  }
+  const uint32_t n = kind == kTopP ? fetch_list(ws, row, sh) : 0u;
+  if (kind == kTopP && n <= kCap) {
     const Cut c = row_cut<kRowWaves>(ws, row, ws.mass(row), r.p, sh);
     if (threadIdx.x < ws.parts) sh.seg[threadIdx.x] = ws.kept(row)[threadIdx.x];
     __syncthreads();
@@ -1079,12 +1068,15 @@ void sample_finish_kernel(SampleArgs g, SampleWs ws) {
 // Host side
 // ---------------------------------------------------------------------------
 constexpr int64_t kSampleMaxCols = 1 << 22;   // sums below 2^62
-// Below kSplitRows rows, rows of two parts or more are split into parts of kPartCols
-// words: with the vectors at both ends at most 8192 elements, as the scan holds.
-constexpr int64_t kPartCols = 8160, kSplitRows = 128;
+// Rows of kSplitCols words or more are split into parts of kPartCols (with the vectors
+// at both ends at most 8192 elements, as the scan holds) up to kSplitRows rows, with a
+// top-p up to half as many: one workgroup a row against the split, binary32, no filter
+// 1 x 50257 14.6 / 15.3 us, 1 x 128256 26.3 / 15.7, 64 x 128256 28.8 / 23.9, 127 x 128256
+// 33.2 / 36.6; top-p 1 x 50257 25.2 / 28.9, 32 x 128256 52.8 / 34.6, 64 x 128256 48.2 / 47.8.
+constexpr int64_t kPartCols = 8160, kSplitCols = 65536, kSplitRows = 64;
 
 static int64_t sample_parts(int64_t rows, int64_t cols) {
-  return rows > 0 && rows < kSplitRows && cols >= 2 * kPartCols ? (cols + kPartCols - 1) / kPartCols : 1;
+  return rows > 0 && rows <= kSplitRows && cols >= kSplitCols ? (cols + kPartCols - 1) / kPartCols : 1;
 }
 static_assert((kSampleMaxCols + kPartCols - 1) / kPartCols <= kMaxSegs, "a segment a part");
 static int64_t sample_row_ws(int64_t parts) {
@@ -1102,7 +1094,7 @@ static void launch_sample(uint32_t n, hipStream_t s, const SampleArgs& g, uint32
     return;
   }
   const dim3 parts(n * ws.parts), b(kPartThreads);
-  hipLaunchKernelGGL((sample_scan_kernel<DT, MODE>), parts, b, 0, s, g, ws);
+  hipLaunchKernelGGL((sample_scan_kernel<DT>), parts, b, 0, s, g, ws);
   hipLaunchKernelGGL((sample_mass_kernel<DT, MODE>), parts, b, 0, s, g, ws);
   if (g.top_p != nullptr)
     hipLaunchKernelGGL((sample_cut_kernel<DT, MODE>), parts, b, 0, s, g, ws);
@@ -1152,9 +1144,10 @@ extern "C" quake_status quake_sample(const void* x, const float* u, int32_t* tok
                      ldx, (uint32_t)cols};
   const int64_t parts = sample_parts(rows, cols);
   SampleWs ws{nullptr, 0, 1};
-  if (workspace != nullptr && parts > 1) {
+  if (workspace != nullptr && workspace_bytes < sample_ws_bytes(rows, parts)) return QUAKE_EINVAL;
+  if (workspace != nullptr && parts > 1 && top_k == nullptr &&
+      (top_p == nullptr || 2 * rows <= kSplitRows)) {
     ws = {static_cast<char*>(workspace), sample_row_ws(parts), (uint32_t)parts};
-    if (workspace_bytes < sample_ws_bytes(rows, parts)) return QUAKE_EINVAL;
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);
   constexpr int64_t kMost = 1 << 20;   // rows a launch: below 2^32 threads

@@ -56,6 +56,9 @@ SHAPES = [
     (1, 64, 640, 2, 1, 64, 100, 2 ** 31 - 1),  # every key a sink
     (2, 257, 700, 6, 3, 128, 1, 0),            # itself alone
     (1, 1500, 1500, 4, 1, 128, 700, 7),
+    (1, 160, 3000, 2, 2, 64, 2500, 3),         # rows that share tiles, keys split
+    (1, 100, 9000, 1, 1, 128, 9000, 0),
+    (1, 97, 600, 1, 1, 64, 500, 100),
 ]
 
 
