@@ -386,7 +386,8 @@ quake_status quake_attention(const void* q, const void* k, const void* vt, void*
  *          contiguous; the other strides, in elements, are in `strides` (host
  *          pointer): of the batch, the token and the head. Each is >= 0 and a
  *          multiple of 8 (of a size of 1: anything), the key and value tokens' at
- *          most 2^24; all pointers 16-byte aligned. o overlaps nothing.
+ *          most 2^24, o's at least dim; all pointers 16-byte aligned. o overlaps nothing,
+ *          none of its rows another.
  *   q_lens, kv_lens : device int32, one per sequence, or NULL (sq, skv): tokens
  *          each sequence has in the padded buffers, clamped to 0 .. sq and
  *          0 .. skv. Queries from q_len on are not read and their o is left as it
@@ -446,9 +447,9 @@ quake_status quake_attention_window(const void* q, const void* k, const void* v,
  *           NaN, min_p <= 0 or NaN: no such filter for the row; top_p <= 0 keeps one
  *           word; min_p > 1 counts as 1.
  *   workspace : device, 16-byte aligned, of the size quake_sample_workspace_size
- *           gives (0: none needed), any content: a row is then read by several
- *           workgroups. NULL: one workgroup per row. Calls that may run at the same
- *           time need workspaces of their own.
+ *           gives (0: none needed), any content: few long rows without a top_k are
+ *           then read by several workgroups each. NULL: one workgroup per row. Calls
+ *           that may run at the same time need workspaces of their own.
  * rows == 0 launches nothing.
  */
 quake_status quake_sample_workspace_size(int64_t rows, int64_t cols, int64_t* bytes);
@@ -488,7 +489,8 @@ quake_status quake_sample(const void* x, const float* u, int32_t* token, float* 
  *          workspaces of their own.
  * Rows are read as the aligned 16-byte vectors that cover them (up to 15 bytes
  * around a row, never outside such a vector) and written inside only. Sums are
- * binary32 within a vector, then binary64 in a fixed order: the same bits every time.
+ * binary32 within four vectors, then binary64 in a fixed order: the same bits every
+ * time (with a workspace others than without).
  * quake_distill_grad is the gradient alone, from the same x, idx, y, mode, t and the
  * stats that quake_distill gave, where its weight is known only later.
  */

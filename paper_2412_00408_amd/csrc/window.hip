@@ -801,15 +801,14 @@ extern "C" quake_status quake_attention_window(
       ((uintptr_t)q_lens & 3u) != 0 || ((uintptr_t)kv_lens & 3u) != 0)
     return QUAKE_EINVAL;
   const quake_window_strides& st = *strides;
-  const int64_t n[4] = {batch, sq, skv, 1};
-  for (int i = 0; i < 3; ++i) {
-    const int64_t count = i == 0 ? batch : i == 1 ? 0 : heads;   // tokens: per operand below
-    for (const int64_t* s : {st.q, st.k, st.v, st.o}) {
-      const bool kv = s == st.k || s == st.v;
-      const int64_t c = i == 1 ? (kv ? n[2] : n[1]) : (i == 2 && kv) ? kv_heads : count;
-      if (c <= 1) continue;   // never multiplied by anything but 0
-      if (s[i] < 0 || s[i] % 8 != 0 || s[i] > INT64_MAX / 8 / c) return QUAKE_EINVAL;
+  for (const int64_t* s : {st.q, st.k, st.v, st.o}) {
+    const bool kv = s == st.k || s == st.v;
+    const int64_t count[3] = {batch, kv ? skv : sq, kv ? kv_heads : heads};
+    for (int i = 0; i < 3; ++i) {
+      if (count[i] <= 1) continue;   // never multiplied by anything but 0
+      if (s[i] < 0 || s[i] % 8 != 0 || s[i] > INT64_MAX / 8 / count[i]) return QUAKE_EINVAL;
       if (i == 1 && kv && s[i] > (1 << 24)) return QUAKE_EINVAL;   // 32-row offsets in 32 bits
+      if (s == st.o && s[i] < dim) return QUAKE_EINVAL;            // rows of o on one another
     }
   }
   const WindowPlan p = window_plan(batch, sq, skv, heads / kv_heads, kv_heads, window, sinks);

@@ -53,7 +53,8 @@ def window(q):
     dict(nws=-1), dict(st=strides(q=(64, 60, 64))), dict(st=strides(k=(64, -64, 64))),
     dict(st=strides(k=(64, (1 << 24) + 8, 64))), dict(st=strides(v=(64, (1 << 24) + 8, 64))),
     dict(st=strides(o=(-8, 64, 64))), dict(st=strides(v=(4, 64, 64))),
-    dict(st=strides(o=(64, 64, 3))), dict(st=strides(q=(BIG, 64, 64))), dict(skv=(1 << 30) + 1),
+    dict(st=strides(o=(64, 64, 3))), dict(st=strides(o=(64, 64, 0))), dict(st=strides(o=(0, 64, 64))),
+    dict(st=strides(o=(64, 56, 64))), dict(st=strides(q=(BIG, 64, 64))), dict(skv=(1 << 30) + 1),
     dict(sq=(1 << 24) + 1), dict(batch=1 << 30), dict(heads=1 << 20, kv=1 << 20)], ids=str)
 def test_window_refusals(q, bad):
     assert window(q)(**bad) == q.EINVAL

@@ -87,6 +87,28 @@ def test_wide_nucleus(q):
     run(q, "wide", x, [0.1, 0.5, 0.7, 0.99], top_p=[0.9, 0.5, 0.99, 0.1], top_k=[0, 90000, 3000, 0])
 
 
+def test_longest_rows(q):
+    x = logits(2, 1 << 22, torch.bfloat16, 21)
+    u = [0.3, 0.8]
+    run(q, "longest", x, u)
+    run(q, "longest top-p", x, u, top_p=[0.9, 0.2], min_p=[0.0, 0.001])
+    run(q, "longest top-k", x, u, top_k=[60, 1], temperature=[0.7, 0.0])
+    run(q, "longest greedy", x, u, temperature=[0.0, 1.0])
+
+
+def test_split_rows_with_greedy_rows_among_them(q):
+    for dt in DTS:
+        x = logits(6, 70001, dt, 22)
+        x[1, 60000:60010] = x[1].max() + 1           # equal largest words
+        x[1, 30:33] = x[1, 60000]
+        x[2] = -math.inf
+        x[3, 5] = math.inf
+        u = [0.1, 0.9, 0.5, 0.5, 0.7, 0.2]
+        temp = [0.0, 0.0, 0.0, 0.0, 1.0, -3.0]
+        run(q, "greedy among", x, u, temperature=temp)
+        run(q, "greedy among, top-p", x, u, temperature=temp, top_p=[0.9] * 6, min_p=[0.02] * 6)
+
+
 def test_masked_words_infinities_and_nan(q):
     inf, nan = math.inf, math.nan
     for cols in (40, 20000, 40000):

@@ -169,6 +169,21 @@ def test_long_cache_token(q):
     check("200000 keys", q.quake_attention_window(*x, t=0.08, workspace=ws), ref)
 
 
+def test_no_keys_and_more_queries_than_keys(q):
+    for sq in (1, 40, 200):
+        x = make(2, sq, 8, 6, 2, 64, torch.float16, 10)
+        o = q.quake_attention_window(x[0], x[1][:, :0], x[2][:, :0], window=5)
+        assert (o == 0).all()
+        ref = ref64.window_attention(*x, 5, 1, 2, 0.125)
+        o = q.quake_attention_window(*x, window=5, sinks=1)
+        check("sq %d over 8 keys" % sq, o, ref)
+        if sq > 8:
+            assert (o[:, :sq - 8] == 0).all()
+    with pytest.raises(q.QuakeError):                # rows of the output on one another
+        x = make(2, 3, 8, 4, 2, 64, torch.float16, 11)
+        q.quake_attention_window(*x, x[0][:, :, :1].clone().expand(2, 3, 4, 64), window=5)
+
+
 def test_same_bits_every_time_on_another_stream_and_in_a_graph(q):
     for sq in (1, 200):
         x = make(2, sq, 900, 8, 2, 128, torch.bfloat16, 8)
