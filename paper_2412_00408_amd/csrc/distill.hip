@@ -324,7 +324,11 @@ __device__ __forceinline__ void row_grad(const DistillArgs& g, uint32_t row, uin
   }
 }
 
-// The whole row by one workgroup.
+// The whole row by one workgroup. 2048 x 128256 bf16: 285 us, 3.7 TB/s of the logits in
+// and the gradient out (the statistics alone 100 us, 5.2 TB/s): the second reading comes
+// from the memory-side cache, and both passes are long enough in VALU work (21
+// instructions an element) that a register-held row, which one compute unit could not
+// compute beside loading, was not built.
 template <int DT, int MODE>
 __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs g, uint32_t row0) {
   __shared__ DistillShared sh;
