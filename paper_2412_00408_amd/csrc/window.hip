@@ -711,20 +711,37 @@ struct WindowPlan {
 // second launch costs more than it saves.
 constexpr int64_t kWinTarget = 256, kSplitKeys = 128, kSplitFrom = 512;
 constexpr int64_t kJoinFew = 8;     // splits up to which D / 4 lanes join a row
-constexpr int64_t kManyRows = 96;   // rows from which on 128 share a workgroup
+
+// From kManyRows rows on, 128 rows share a workgroup, unless workgroups of 32 rows fit
+// one to a compute unit and each walks at most kFewWalk keys: what sharing saves is
+// then no compute unit's time, while a short walk's start and end are longer for it.
+// 32 rows against 128 (us; heads dim 128 unless said): 300 to 380 rows x 8 key heads,
+// 2000 keys, 13.9 to 19.4 / 21.8 to 24.4; 256 rows x 8, 4096 keys (walk 1024) 18.5 /
+// 24.0; 128 x 16 x 100 keys at dim 64 5.3 / 7.6; 128 x 64, 512 keys 16.0 / 21.2, 1024
+// keys 25.0 / 21.4 (the one found that loses within the limit); a walk of 2040 keys
+// 43 / 26, of 4096 83 / 37. Several workgroups of 32 rows a compute unit lose where
+// there are many (384: 61 / 34, 768: 233 / 125), though not always (512 over 512 causal
+// keys: 18.3 / 24.3).
+constexpr int64_t kManyRows = 96, kFewWalk = 1024;
 
 static WindowPlan window_plan(int64_t batch, int64_t sq, int64_t skv, int64_t group,
                               int64_t kv_heads, int64_t window, int64_t sinks) {
   WindowPlan p;
   const int64_t rows = sq * group;
   p.tiles = (rows + 31) / 32;
-  p.many = rows >= kManyRows;
-  const int64_t wide = p.many ? 128 : 32;
-  const int64_t items = batch * kv_heads * ((rows + wide - 1) / wide);
-  const int64_t queries = (wide - 1 + group) / group;   // most positions a tile covers, less one
-  const int64_t keys = std::min(skv, std::min(window, skv) + std::min(sinks, skv) + queries);
-  const int64_t most = keys < kSplitFrom ? 1 : keys / kSplitKeys;
-  p.nsplit = items == 0 ? 1 : std::max<int64_t>(1, std::min(most, kWinTarget / items));
+  int64_t walk = 0;   // keys of one workgroup
+  const auto split = [&](int64_t wide) {
+    const int64_t items = batch * kv_heads * ((rows + wide - 1) / wide);
+    const int64_t queries = (wide - 1 + group) / group;   // most positions a tile covers, less one
+    const int64_t keys = std::min(skv, std::min(window, skv) + std::min(sinks, skv) + queries);
+    const int64_t most = keys < kSplitFrom ? 1 : keys / kSplitKeys;
+    p.nsplit = items == 0 ? 1 : std::max<int64_t>(1, std::min(most, kWinTarget / items));
+    walk = keys / p.nsplit;
+    return items;
+  };
+  p.many = false;
+  if (split(32) > kWinTarget || walk > kFewWalk) p.many = rows >= kManyRows;
+  if (p.many) split(128);
   return p;
 }
 

@@ -220,3 +220,69 @@ def test_agrees_with_attention(q):
     ref = ref64.window_attention(*x, 2 ** 31 - 1, 0, 0, 0.125)
     check("window", o, ref)
     check("attention", a.transpose(0, 1)[None], ref)
+
+
+# From 96 rows a key head on, the sequences repeated until workgroups of 32 rows outnumber
+# the compute units, and long walks of few rows: the form with 128 rows a workgroup.
+def repeats(shape):
+    b, sq, _, h, hk = shape[:5]
+    return 1 + 256 // (b * hk * -(-sq * (h // hk) // 32))
+
+
+LARGE = [s for s in SHAPES if s[1] * s[3] // s[4] >= 96] + [
+    (1, 130, 200, 4, 4, 128, 2 ** 31 - 1, 0),
+    (1, 100, 9000, 8, 8, 64, 9000, 0),         # 32 workgroups share a tile's keys
+    (1, 128, 9000, 8, 8, 128, 8500, 9),
+]
+
+
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+@pytest.mark.parametrize("dt", HALF, ids=["bf16", "f16"])
+def test_many_rows(q, shape, dt):
+    b, sq, skv, h, hk, d, window, sinks = shape
+    one = make(b, sq, skv, h, hk, d, dt, 11)
+    n = 1 if hk * skv > 50000 else repeats(shape)
+    x = [a.repeat(n, 1, 1, 1) for a in one]
+    t = 1.0 / math.sqrt(d)
+    for mode in (0, 1, 2, 3):
+        ref = ref64.window_attention(*one, window, sinks, mode, t)
+        for ws in (None, q.attention_window_workspace(x[0], x[1], window, sinks)):
+            o = q.quake_attention_window(*x, window=window, sinks=sinks, mode=mode, workspace=ws)
+            check("many rows %s %s mode %d %s" % (shape, dt, mode, ws is not None), o[:b], ref)
+            assert torch.equal(o.view(n, -1), o[:b].reshape(1, -1).expand(n, -1))
+
+
+def test_many_rows_with_scores_that_keep_rising_and_ragged_lengths(q):
+    for dt in HALF:
+        x = make(32, 70, 640, 8, 4, 64, dt, 12)      # 640 workgroups of 32 rows
+        ramp = torch.linspace(-1, 1, 640, device="cuda")[None, :, None, None]
+        up = (torch.ones_like(x[0]) * 3).to(dt)
+        kl = torch.arange(0, 640, 20, dtype=torch.int32, device="cuda")
+        ql = torch.arange(70, 6, -2, dtype=torch.int32, device="cuda")
+        for scale in (0.5, 4.0, -4.0):
+            k = (x[1].float() * 0.1 + ramp * scale).to(dt)
+            for lens in ((None, None), (ql, kl)):
+                ref = ref64.window_attention(up, k, x[2], 600, 4, 2, 0.5, *lens)
+                o = torch.full_like(x[0], 7.0)
+                q.quake_attention_window(up, k, x[2], o, window=600, sinks=4, t=0.5, q_lens=lens[0],
+                                         kv_lens=lens[1])
+                check("many rows, ramp %s %s %s" % (dt, scale, lens[0] is not None), o, ref)
+                assert (o[~ref[2]] == 7.0).all()
+
+
+def test_many_rows_same_bits_in_a_graph(q):
+    x = make(6, 200, 900, 8, 2, 128, torch.bfloat16, 13)   # 300 workgroups of 32 rows
+    ws = q.attention_window_workspace(x[0], x[1], 500, 4)
+    assert ws is not None
+    eager = q.quake_attention_window(*x, window=500, sinks=4, workspace=ws)
+    o = torch.empty_like(eager)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        q.quake_attention_window(*x, o, window=500, sinks=4, workspace=ws)
+    for _ in range(4):
+        o.zero_()
+        graph.replay()
+        again = q.quake_attention_window(*x, window=500, sinks=4, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(o, eager) and torch.equal(again, eager)
