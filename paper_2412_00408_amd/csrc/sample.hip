@@ -789,7 +789,8 @@ __device__ __forceinline__ uint32_t weigh_list(uint32_t n, float m, const RowPar
 
 // One workgroup per row: every pass after the first finds the row in the caches. 64 x
 // 128256 binary32 with a top-k 21.6 us (1.5 TB/s), bound by one compute unit's loads;
-// 256 x 50257 bf16 with a top-p 26 us, bound by its VALU (about 45 instructions a word).
+// 256 x 50257 bf16 with a top-p 26 us at temperature 1 and 0.9, 36 us with both drawn row
+// by row, bound by its VALU (about 45 instructions a word).
 template <int DT, int MODE>
 __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void sample_row_kernel(SampleArgs g, uint32_t row0) {
