@@ -399,8 +399,8 @@ quake_status quake_attention(const void* q, const void* k, const void* vt, void*
  *          needed), any content; a call's keys are then split over more
  *          workgroups. NULL: never split. Calls that may run at the same time need
  *          workspaces of their own.
- *   batch <= 2^24, sq <= 2^24, skv <= 2^30, heads <= 2^16, and at most 2^24 tiles
- *   of 32 rows (a row: one query of one head); dtype QUAKE_BF16 or QUAKE_F16 (else
+ *   batch <= 2^24, sq <= 2^24, skv <= 2^30, heads <= 2^16, and fewer than 2^24 tiles
+ *   of 32 rows of one key head (a row: one query of one head); dtype QUAKE_BF16 or QUAKE_F16 (else
  *   QUAKE_EDTYPE); t as in quake_attention. batch == 0 or sq == 0 launches nothing.
  * A visible key or value that is not finite may spoil the outputs of other queries
  * of its sequence and key head, those that do not see it among them.

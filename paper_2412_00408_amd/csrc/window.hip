@@ -758,7 +758,8 @@ static bool window_shape_ok(int64_t batch, int64_t sq, int64_t skv, int64_t head
   if (window > INT32_MAX || sinks > INT32_MAX || skv > (1 << 30) || sq > (1 << 24)) return false;
   if (heads > (1 << 16) || batch > (1 << 24)) return false;
   if (sq * (heads / kv_heads) > (1 << 30)) return false;
-  return batch * kv_heads * ((sq * (heads / kv_heads) + 31) / 32) <= (1 << 24);
+  // a workgroup of 256 threads a tile: a launch takes fewer than 2^32 threads
+  return batch * kv_heads * ((sq * (heads / kv_heads) + 31) / 32) < (1 << 24);
 }
 
 template <int DT, int MODE, int D>
