@@ -386,8 +386,9 @@ quake_status quake_attention(const void* q, const void* k, const void* vt, void*
  *          contiguous; the other strides, in elements, are in `strides` (host
  *          pointer): of the batch, the token and the head. Each is >= 0 and a
  *          multiple of 8 (of a size of 1: anything), the key and value tokens' at
- *          most 2^24, o's at least dim; all pointers 16-byte aligned. o overlaps nothing,
- *          none of its rows another.
+ *          most 2^24; o's, in ascending order, each at least what the smaller ones
+ *          span (dim, then (size - 1) strides more), so that no row of o meets another;
+ *          all pointers 16-byte aligned. o overlaps nothing.
  *   q_lens, kv_lens : device int32, one per sequence, or NULL (sq, skv): tokens
  *          each sequence has in the padded buffers, clamped to 0 .. sq and
  *          0 .. skv. Queries from q_len on are not read and their o is left as it

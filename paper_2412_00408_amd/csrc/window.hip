@@ -762,6 +762,22 @@ static bool window_shape_ok(int64_t batch, int64_t sq, int64_t skv, int64_t head
   return batch * kv_heads * ((sq * (heads / kv_heads) + 31) / 32) < (1 << 24);
 }
 
+// Whether no row of o shares elements with another: in ascending order each stride
+// reaches past what the smaller ones span. (Layouts that interleave otherwise without
+// meeting are refused as well; no view of a larger tensor by slices and permutations
+// is one.)
+static bool rows_apart(const int64_t (&stride)[3], const int64_t (&count)[3], int64_t dim) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+  int64_t span = dim;
+  for (const int i : order) {
+    if (count[i] <= 1) continue;
+    if (stride[i] < span) return false;
+    span += stride[i] * (count[i] - 1);
+  }
+  return true;
+}
+
 template <int DT, int MODE, int D>
 static void launch_window(bool many, int64_t heads, hipStream_t s, const WindowArgs& g) {
   const int64_t wide = many ? kWinWaves : 1;   // tiles of 32 rows a workgroup
@@ -830,8 +846,8 @@ extern "C" quake_status quake_attention_window(
       if (count[i] <= 1) continue;   // never multiplied by anything but 0
       if (s[i] < 0 || s[i] % 8 != 0 || s[i] > INT64_MAX / 8 / count[i]) return QUAKE_EINVAL;
       if (i == 1 && kv && s[i] > (1 << 24)) return QUAKE_EINVAL;   // 32-row offsets in 32 bits
-      if (s == st.o && s[i] < dim) return QUAKE_EINVAL;            // rows of o on one another
     }
+    if (s == st.o && !rows_apart(st.o, count, dim)) return QUAKE_EINVAL;
   }
   const WindowPlan p = window_plan(batch, sq, skv, heads / kv_heads, kv_heads, window, sinks);
   const int64_t need = window_ws_bytes(p, batch, kv_heads, dim);
