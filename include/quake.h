@@ -398,7 +398,8 @@ quake_status quake_attention(const void* q, const void* k, const void* vt, void*
  *   workspace : device, 16-byte aligned, of the size that
  *          quake_attention_window_workspace_size gives for these sizes (0: none
  *          needed), any content; a call's keys are then split over more
- *          workgroups. NULL: never split. Calls that may run at the same time need
+ *          workgroups. NULL: never split. It lies outside the bytes from the first to
+ *          the last of every operand. Calls that may run at the same time need
  *          workspaces of their own.
  *   batch <= 2^24, sq <= 2^24, skv <= 2^30, heads <= 2^16, and fewer than 2^24 tiles
  *   of 32 rows of one key head (a row: one query of one head); dtype QUAKE_BF16 or QUAKE_F16 (else
@@ -449,7 +450,8 @@ quake_status quake_attention_window(const void* q, const void* k, const void* v,
  *           word; min_p > 1 counts as 1.
  *   workspace : device, 16-byte aligned, of the size quake_sample_workspace_size
  *           gives (0: none needed), any content: few long rows without a top_k are
- *           then read by several workgroups each. NULL: one workgroup per row. Calls
+ *           then read by several workgroups each. NULL: one workgroup per row. It
+ *           lies outside the bytes from the first to the last of every operand. Calls
  *           that may run at the same time need workspaces of their own.
  * rows == 0 launches nothing.
  */
@@ -486,7 +488,8 @@ quake_status quake_sample(const void* x, const float* u, int32_t* token, float* 
  *   quake_softmax. Logits of +inf or NaN: unspecified. |t x| below 1e6.
  *   workspace : device, 16-byte aligned, of the size quake_distill_workspace_size
  *          gives (0: none needed), any content: few rows are then cut into chunks.
- *          NULL: one workgroup per row. Calls that may run at the same time need
+ *          NULL: one workgroup per row. It lies outside the bytes from the first to
+ *          the last of every operand. Calls that may run at the same time need
  *          workspaces of their own.
  * Rows are read as the aligned 16-byte vectors that cover them (up to 15 bytes
  * around a row, never outside such a vector) and written inside only. Sums are

@@ -508,6 +508,13 @@ extern "C" quake_status quake_distill(const void* x, const int32_t* idx, const v
                 (uint32_t)cols, (uint32_t)topk, 1u, (int32_t)ydtype, c0, t};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (workspace != nullptr && need > 0) {
+    if (meet(workspace, need, x, rows_bytes(rows, cols, ldx, elem_size(dtype))) ||
+        meet(workspace, need, grad, rows_bytes(rows, cols, ldg, elem_size(dtype))) ||
+        meet(workspace, need, idx, rows_bytes(rows, topk, ldi, 4)) ||
+        meet(workspace, need, y, rows_bytes(rows, topk, ldy, elem_size(ydtype))) ||
+        meet(workspace, need, weight, 4 * rows) || meet(workspace, need, loss, 4 * rows) ||
+        meet(workspace, need, stats, 8 * rows))
+      return QUAKE_EINVAL;
     g.chunks = (uint32_t)distill_chunks(rows, cols);
     if (g.stats == nullptr)
       g.stats = reinterpret_cast<float*>(static_cast<char*>(workspace) + rows * 16 * g.chunks);

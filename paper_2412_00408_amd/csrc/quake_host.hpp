@@ -58,6 +58,16 @@ inline int64_t elem_size(int d) { return d == QUAKE_F32 ? 4 : 2; }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
+// Whether bytes [a, a + na) and [b, b + nb) meet (a null pointer has none).
+inline bool meet(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a != nullptr && b != nullptr && na > 0 && nb > 0 && x < y + (uint64_t)nb && y < x + (uint64_t)na;
+}
+// Bytes from the first to behind the last of rows x cols elements, rows ld apart.
+inline int64_t rows_bytes(int64_t rows, int64_t cols, int64_t ld, int64_t elem) {
+  return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * elem : 0;
+}
+
 inline quake_status launch_status() {
   return hipGetLastError() == hipSuccess ? QUAKE_OK : QUAKE_EHIP;
 }

@@ -1152,6 +1152,11 @@ extern "C" quake_status quake_sample(const void* x, const float* u, int32_t* tok
   if (workspace != nullptr && workspace_bytes < sample_ws_bytes(rows, parts)) return QUAKE_EINVAL;
   if (workspace != nullptr && parts > 1 && top_k == nullptr &&
       (top_p == nullptr || 2 * rows <= kSplitRows)) {
+    const int64_t need = sample_ws_bytes(rows, parts);
+    if (meet(workspace, need, x, rows_bytes(rows, cols, ldx, elem_size(dtype)))) return QUAKE_EINVAL;
+    for (const void* p : {(const void*)u, (const void*)token, (const void*)prob,
+                          (const void*)temperature, (const void*)top_p, (const void*)min_p})
+      if (meet(workspace, need, p, 4 * rows)) return QUAKE_EINVAL;
     ws = {static_cast<char*>(workspace), sample_row_ws(parts), (uint32_t)parts};
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -852,7 +852,21 @@ extern "C" quake_status quake_attention_window(
   const WindowPlan p = window_plan(batch, sq, skv, heads / kv_heads, kv_heads, window, sinks);
   const int64_t need = window_ws_bytes(p, batch, kv_heads, dim);
   const bool split = workspace != nullptr && need > 0;
-  if (split && workspace_bytes < need) return QUAKE_EINVAL;
+  if (split) {
+    if (workspace_bytes < need) return QUAKE_EINVAL;
+    const auto bytes = [&](const int64_t (&s)[3], int64_t tokens, int64_t n) {
+      const int64_t count[3] = {batch, tokens, n};
+      int64_t last = dim;
+      for (int i = 0; i < 3; ++i) last += count[i] > 1 ? s[i] * (count[i] - 1) : 0;
+      return tokens > 0 ? 2 * last : 0;
+    };
+    if (meet(workspace, need, q, bytes(st.q, sq, heads)) ||
+        meet(workspace, need, k, bytes(st.k, skv, kv_heads)) ||
+        meet(workspace, need, v, bytes(st.v, skv, kv_heads)) ||
+        meet(workspace, need, o, bytes(st.o, sq, heads)) ||
+        meet(workspace, need, q_lens, 4 * batch) || meet(workspace, need, kv_lens, 4 * batch))
+      return QUAKE_EINVAL;
+  }
   WindowArgs g{};
   g.q = static_cast<const uint16_t*>(q);
   g.k = static_cast<const uint16_t*>(k);
