@@ -380,7 +380,9 @@ quake_status quake_attention(const void* q, const void* k, const void* vt, void*
  * common factor per row and that factor's place in the period of the
  * approximation's error; each is within the mode's error of e^(t s).
  * Probabilities are rounded to the 16-bit format before the second product and
- * their sum, which are binary32; the quotient is rounded once.
+ * their sum, which are binary32 (binary16's to its 11 digits down to 2^-20 of the
+ * row's largest, smaller ones to 2^-31 of the largest); the quotient is rounded
+ * once.
  *   q, o : device, batch x sq tokens x heads x dim, dtype; k, v : device,
  *          batch x skv tokens x kv_heads x dim, dtype. dim (64 or 128) is
  *          contiguous; the other strides, in elements, are in `strides` (host

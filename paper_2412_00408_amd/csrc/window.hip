@@ -10,8 +10,9 @@
 // keys are read once, and partial results of different keys join exactly,
 // whatever their number and order. c1 = (127 - M) 2^23 is exact in binary32, so
 // l = fma(s, c0, c1) has one rounding. M follows the running max lazily, only
-// when it falls more than kLazy below (probabilities then reach 2^kLazy, which
-// binary32 sums and both 16-bit formats hold with the same relative rounding).
+// when it falls more than kLazy below (probabilities then reach 2^kLazy, binary16's
+// 2^(kLift + kLazy), which binary32 sums and both 16-bit formats hold with the same
+// relative rounding).
 //
 // Rows. The queries of all heads that share a key head are one list of rows,
 // row r = query r / group, head r mod group of the group, so a single token's
@@ -44,7 +45,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr float kLazy = 8.0f;      // how far the running max may rise above M
+constexpr float kLazy = 8.0f;      // how far the running max may rise before M follows
+// A largest probability is held at 2^kLift or below when M is set: binary16's steps end
+// at 2^-24, and held against 1 keys of 2^-14 of the largest and less would lose digits,
+// those below 2^-25 all of them (a sink over thousands of keys). 2^(kLift + kLazy) fits.
+template <int DT>
+constexpr float kLift = DT == F16 ? 7.0f : 0.0f;
 constexpr float kNoMax = -1e30f;   // M of a row that has seen no key
 constexpr int kWinWaves = 4;
 
@@ -192,11 +198,11 @@ __device__ __forceinline__ float block_top(const f32x16& s, float c0) {
   for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
   return fmaxf(top, other_half(top)) * (c0 * (MODE == EXACT ? 1.0f : 0x1p-23f));
 }
-// M raised to `top` where that is more than `lazy` above it, and what is accumulated
-// rescaled; returns the exponent it was rescaled by.
-template <int D>
-__device__ __forceinline__ int32_t raise_max(float top, float lazy, RowAcc<D>& acc) {
-  const float m = top > acc.m + lazy ? __builtin_ceilf(top) : acc.m;
+// M brought to kLift below `top` where that is more than kLazy further above it, and what
+// is accumulated rescaled; returns the exponent it was rescaled by.
+template <int DT, int D>
+__device__ __forceinline__ int32_t raise_max(float top, RowAcc<D>& acc) {
+  const float m = top > acc.m + (kLift<DT> + kLazy) ? __builtin_ceilf(top) - kLift<DT> : acc.m;
   const int32_t e = down_shift(acc.m, m);
   acc.m = m;
   acc.sum = __builtin_amdgcn_ldexpf(acc.sum, e);
@@ -317,7 +323,7 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
     for (int ks = 0; ks < D / 16; ++ks) s = wmma<DT>(read_k<D>(kblk, fr, h, ks), qf[ks], s);
     if (!all_seen(sp, 32 * n, first, last, g)) mask_block(s, sp, 32 * n, pos, h, g);
     const float top = block_top<MODE>(s, g.c0);
-    if (__any(top > acc.m + kLazy)) raise_max(top, kLazy, acc);
+    if (__any(top > acc.m + (kLift<DT> + kLazy))) raise_max<DT>(top, acc);
     const float c1 = row_c1<MODE>(acc.m);
     u32x4 p[2];
 #pragma unroll
@@ -520,10 +526,10 @@ __global__ __launch_bounds__(64 * kWinWaves, 2) void window_many_kernel(WindowAr
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
     if (__any(top > limit)) {
-      const int32_t e = raise_max(fmaxf(top, other_half(top)) * units, kLazy, acc);
+      const int32_t e = raise_max<DT>(fmaxf(top, other_half(top)) * units, acc);
 #pragma unroll
       for (int i = 0; i < 8; ++i) pp[i >> 2][i & 3] = scale_pair<DT>(pp[i >> 2][i & 3], e);
-      limit = (acc.m + kLazy) / units;
+      limit = (acc.m + (kLift<DT> + kLazy)) / units;
     }
     const float c1 = row_c1<MODE>(acc.m);
 #pragma unroll
