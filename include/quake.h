@@ -375,10 +375,14 @@ quake_status quake_attention(const void* q, const void* k, const void* vt, void*
  * query head n reads key head n / (heads / kv_heads).
  * The exponentials are taken against a whole number M of base-2 units, not the
  * row max of Algorithm 2: QuAKE(y - M) = 2^-M QuAKE(y) exactly for a whole M
- * (Eq. 3: M moves the exponent field only), so partial results join exactly and
- * the keys are read once. They are the values Algorithm 2's would have up to one
- * common factor per row and that factor's place in the period of the
- * approximation's error; each is within the mode's error of e^(t s).
+ * (Eq. 3: M moves the exponent field only), so partial results are brought to one M
+ * by exact powers of two and the keys are read once. They are the values Algorithm
+ * 2's would have up to one common factor per row and that factor's place in the
+ * period of the approximation's error; each is within the mode's error of e^(t s).
+ * Arguments are rounded at the M of their time and sums in the order of the keys:
+ * the same call gives the same bits every time, with a workspace others than
+ * without. |t q.k| below 1e6 (beyond it M is no longer exact; NaN and rows of
+ * zeros are possible).
  * Probabilities are rounded to the 16-bit format before the second product and
  * their sum, which are binary32 (binary16's to its 11 digits down to 2^-20 of the
  * row's largest, smaller ones to 2^-31 of the largest); the quotient is rounded

@@ -7,12 +7,15 @@
 // the bit constructions too, as M only moves the exponent field (l of Eq. 5 moves
 // by M 2^23, its mantissa bits stay). So here, unlike in Algorithm 2 with its
 // real-valued max, a running M can be raised later by an exact power of two: the
-// keys are read once, and partial results of different keys join exactly,
-// whatever their number and order. c1 = (127 - M) 2^23 is exact in binary32, so
-// l = fma(s, c0, c1) has one rounding. M follows the running max lazily, only
-// when it falls more than kLazy below (probabilities then reach 2^kLazy, binary16's
-// 2^(kLift + kLazy), which binary32 sums and both 16-bit formats hold with the same
-// relative rounding).
+// keys are read once, and partial results of different keys are brought to one M
+// without an error, whatever their number. (Roundings stay: l's at the M of its time,
+// the 16-bit ones, and those of binary32 sums in their order.) c1 = (127 - M) 2^23 is
+// exact in binary32 for |M| < 2^23, which |t q.k| < 1e6 keeps far from, so
+// l = fma(s, c0, c1) has one rounding; M is then off by less than 1/8 unit of the row's
+// max, which binary16's largest probability, 2^15, has room for. M follows the
+// running max lazily, only when it falls more than kLazy below (probabilities then
+// reach 2^kLazy, binary16's 2^(kLift + kLazy), which binary32 sums and both 16-bit
+// formats hold with the same relative rounding).
 //
 // Rows. The queries of all heads that share a key head are one list of rows,
 // row r = query r / group, head r mod group of the group, so a single token's

@@ -1,6 +1,7 @@
-"""quake_attention_window where its probabilities are far apart: binary16 rows whose sink
-takes the row max while thousands of keys lie far below it. Scores are products that
-binary32 holds exactly, so the references below need no bound for them."""
+"""quake_attention_window where its probabilities or scores are far apart: scores up
+to the stated |t q.k| of 1e6, and binary16 rows whose sink takes the row max while
+thousands of keys lie far below it. Scores are sums of two products that binary32
+holds exactly, so the references below need no bound for them."""
 import math
 
 import numpy as np
@@ -11,6 +12,7 @@ import ref64
 from gpu_util import say
 
 pytestmark = pytest.mark.gpu
+HALF = [torch.bfloat16, torch.float16]
 
 
 @pytest.fixture(scope="module")
@@ -74,6 +76,29 @@ def gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
 
+@pytest.mark.parametrize("dt", HALF, ids=["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sq", [1, 120])
+def test_scores_up_to_the_stated_bound(q, dt, d, sq):
+    skv, t = 600, 0.125
+    g = gen(d + sq)
+    fine = torch.randint(-128, 128, (skv,), generator=g, device="cuda").float() / 2   # t s: 8 either way
+    v = torch.randn((skv, d), generator=g, device="cuda").to(dt)
+    qq = torch.zeros((sq, d), device="cuda")
+    qq[:, 0], qq[:, 1] = 2048.0, 1.0                 # t q.k = 256 k_0 + k_1 / 8
+    ramp = torch.arange(skv, device="cuda") // 60    # 0 .. 9
+    # about 999424 = 256 * 3904 all over, or the row max rising to that from far below
+    for name, base in (("high", torch.full((skv,), 3904.0, device="cuda")),
+                       ("low", torch.full((skv,), -3904.0, device="cuda")),
+                       ("last", torch.where(ramp < 9, -3904.0, 3904.0)),
+                       ("first", torch.where(ramp > 0, -3904.0, 3904.0)),
+                       ("rising", (ramp.float() - 5.0) * 768.0)):
+        k = torch.zeros((skv, d), device="cuda")
+        k[:, 0], k[:, 1] = base, fine
+        for mode in (0, 1, 2, 3):
+            both(q, "scores " + name, qq.to(dt), k.to(dt), v, dt, mode, t, 10 ** 6)
+
+
 @pytest.mark.parametrize("far", [10.0, 15.5, 18.0, 20.0])
 @pytest.mark.parametrize("sq", [1, 120])
 def test_binary16_sinks_far_above_the_other_keys(q, far, sq):
@@ -114,3 +139,16 @@ def test_binary16_keys_of_one_weight_far_below_their_sink(q, far, sq):
     v[0, 1:] = 0.0
     for mode in (0, 1, 2, 3):
         both(q, "one weight %s" % far, qq.to(dt), k.to(dt), v.to(dt), dt, mode, 1.0, 8700, 1)
+
+
+@pytest.mark.parametrize("dt", HALF, ids=["bf16", "f16"])
+def test_many_rows_that_could_be_split_without_a_workspace(q, dt):
+    # 128 rows of each of 4 key heads over 9000 keys: 16 workgroups of 32 rows, each
+    # walking all of them where the call has no workspace
+    g = gen(3)
+    x = [torch.randn(s, generator=g, device="cuda").to(dt)
+         for s in ((1, 64, 8, 64), (1, 9000, 4, 64), (1, 9000, 4, 64))]
+    want, bound, _ = ref64.window_attention(*x, 8000, 5, 2, 0.125)
+    for ws in (None, q.attention_window_workspace(x[0], x[1], 8000, 5)):
+        o = q.quake_attention_window(*x, window=8000, sinks=5, t=0.125, workspace=ws)
+        check("unsplit %s %s" % (dt, ws is None), o, want, bound)
