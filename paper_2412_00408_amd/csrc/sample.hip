@@ -787,10 +787,15 @@ __device__ __forceinline__ uint32_t weigh_list(uint32_t n, float m, const RowPar
                                     : weigh_some<MODE, kCap / kRowThreads>(n, m, p, sh);
 }
 
-// One workgroup per row: every pass after the first finds the row in the caches. 64 x
-// 128256 binary32 with a top-k 21.6 us (1.5 TB/s), bound by one compute unit's loads;
-// 256 x 50257 bf16 with a top-p 26 us at temperature 1 and 0.9, 36 us with both drawn row
-// by row, bound by its VALU (about 45 instructions a word).
+// One workgroup per row: every pass after the first finds most of the row in L2 (1.05 to
+// 1.2 readings past it by the counters). 64 x 128256 binary32 with a top-k 21.6 to 23 us
+// (1.4 TB/s), bound by one compute unit's loads; 256 x 50257 bf16 with a top-p 26 us at
+// temperature 1 and 0.9, 36 us with both drawn row by row, bound by its VALU (67
+// instructions a word in three passes). Rows that overflow the candidates take longer
+// (64 x 128256 binary32, top-k 500 49 us, 900 200 us, 1100 and more 290 us; a top-p of 0.9
+// over logits of standard deviation 3, 0.5, 0.05 and 0 67, 300, 440 and 660 us; a top-k
+// over words masked by the type's lowest value, where fewer lanes than k hold others, 360
+// to 510 us, by -inf 20 us).
 template <int DT, int MODE>
 __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(4, 4)))
 void sample_row_kernel(SampleArgs g, uint32_t row0) {
@@ -859,8 +864,9 @@ void sample_row_kernel(SampleArgs g, uint32_t row0) {
 //   mass    top-p rows: the bins; unranked rows: the parts' kept masses
 //   cut     top-p rows: the cut bin's candidates and the parts' kept masses
 //   finish  the token
-// (With a top-k one workgroup a row was faster at every size: two passes of a compare
-// a word and one launch, 22 against 26 us for 64 x 128256 binary32.)
+// (With a top-k this form had a launch that did nothing for such rows, and one workgroup
+// a row was faster at every size: two passes of a compare a word and one launch, 22
+// against 26 us for 64 x 128256 binary32.)
 // ---------------------------------------------------------------------------
 constexpr int kPartThreads = 256, kPartWaves = 4;
 constexpr uint32_t kWsCap = 16384;       // candidates of a row in the workspace

@@ -261,7 +261,8 @@ __device__ __forceinline__ int32_t seq_len(const int32_t* lens, int b, int32_t m
 // keys and join at the end. What bounds it is reading the keys (single tokens),
 // so each wave keeps the next block's K and V in flight. One token for each of 64
 // caches of up to 8192 (window 4096, 32 heads over 8, head dim 128, bf16): 164 us,
-// 5.5 TB/s; for one cache of 8192 tokens (32 splits) 11 us, 3.0 TB/s.
+// 5.5 TB/s; for one cache of 8192 tokens (32 splits) 10.8 us, 3.1 TB/s, and 3.8 us to
+// join them.
 template <int DT, int MODE, int D>
 __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g) {
   constexpr int kBlk = 64 * D;                      // bytes of a block of 32 rows
@@ -409,8 +410,10 @@ __global__ __launch_bounds__(64 * kWinWaves) void window_few_kernel(WindowArgs g
 // are done with, so the loads of two tiles on start there.
 // What bounds it is VALU issue, so whether M has to rise is asked of each lane's own
 // scores; only if so are the two halves of a row brought together. A prompt of 16384
-// tokens (window 4096, 32 heads over 8, head dim 128, bf16): 1.03 ms, 0.94 PFLOP/s;
-// products take 47 % of the cycles and VALU instructions 51 %, and they hardly overlap.
+// tokens (window 4096, 32 heads over 8, head dim 128, bf16): 1.00 to 1.04 ms, 0.93 to
+// 0.96 PFLOP/s; products take 49 % of the cycles and VALU instructions 53 %, and they
+// hardly overlap. The operand reads from LDS, by count 16 cycles a wave for two products,
+// take nearly as many as both.
 constexpr int kManyKeys = 64;
 
 template <int DT, int MODE, int D>
@@ -730,7 +733,10 @@ constexpr int64_t kJoinFew = 8;     // splits up to which D / 4 lanes join a row
 // keys 25.0 / 21.4 (the one found that loses within the limit); a walk of 2040 keys
 // 43 / 26, of 4096 83 / 37. Several workgroups of 32 rows a compute unit lose where
 // there are many (384: 61 / 34, 768: 233 / 125), though not always (512 over 512 causal
-// keys: 18.3 / 24.3).
+// keys: 18.3 / 24.3). The walk is that of the split call also where a call has no
+// workspace: its few workgroups then walk all keys, which 32 rows, whose four waves share
+// them, do best (64 queries of 8 heads over 4, 9000 keys, dim 64, 54.5 / 149; 16 of 64
+// over 8, 4096 keys, 34.6 / 87.5).
 constexpr int64_t kManyRows = 96, kFewWalk = 1024;
 
 static WindowPlan window_plan(int64_t batch, int64_t sq, int64_t skv, int64_t group,
