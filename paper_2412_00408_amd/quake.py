@@ -416,9 +416,10 @@ def quake_attention_window(q, k, v, o=None, window=2**31 - 1, sinks=0, q_lens=No
     float16 q [batch, sq, heads, dim] and k, v [batch, skv, kv_heads, dim], dim 64
     or 128 contiguous, other strides multiples of 8; heads a multiple of kv_heads.
     q_lens, kv_lens: int32 [batch], the tokens each sequence has (default all);
-    rows of o past q_lens keep what they held (a new o: undefined). t defaults to
-    1/sqrt(dim). `workspace` (from attention_window_workspace) lets a call with few
-    rows split its keys over more workgroups."""
+    rows of o past q_lens keep what they held (a new o: undefined), and no row of o
+    may meet another. t defaults to 1/sqrt(dim); |t q.k| below 1e6. `workspace` (from
+    attention_window_workspace; apart from every operand) lets a call with few rows
+    split its keys over more workgroups."""
     dev, dt = q.get_device(), q.dtype
     for a, what in ((q, "q"), (k, "k"), (v, "v")):
         _operand(a, what, dev)
