@@ -68,7 +68,7 @@
 extern "C" {
 #endif
 
-#define QUAKE_ABI_VERSION 6
+#define QUAKE_ABI_VERSION 7
 
 typedef enum {
   QUAKE_F32 = 0,  /* IEEE binary32 */
@@ -427,6 +427,106 @@ quake_status quake_attention_window(const void* q, const void* k, const void* v,
                                     int64_t window, int64_t sinks, quake_dtype dtype,
                                     quake_mode mode, float t, void* workspace,
                                     int64_t workspace_bytes, void* stream);
+
+/*
+ * quake_attention_shared — attention of a batch whose sequences share a prefix, and the
+ * attention weight that the keys of the sequences' own caches gather. The batch is `groups`
+ * runs of batch / groups sequences; a run's sequences share the keys and values of one
+ * prefix (a system prompt, a document, the prompt of several samples), which are read once
+ * for all of them. Sequence b of group g:
+ *   o_i = sum_j p_ij v_j / sum_j p_ij  over the keys that query i sees: all keys
+ *   j < prefix_len_g of its prefix, and its own keys j <= pos_i, pos_i = kv_len - q_len + i
+ *   (the queries are the last tokens of the own keys),
+ *   weight[b, h, j] += sum_i p_ij / sum_j p_ij  over the queries of all heads that share
+ *   key head h, for the own keys j < kv_len (weight != NULL): what quake_cache_evict goes by.
+ * p_ij = the exponential of `mode` of t q_i.k_j, taken against a whole number of base-2
+ * units as in quake_attention_window, with the same roundings, range of scores (|t q.k|
+ * below 1e6) and grouped heads. `weight` is computed in binary32 from exponentials that are
+ * not rounded to 16 bits. A query that sees no key gets zeros and adds no weight.
+ *   q, o : device, batch x sq tokens x heads x dim, dtype; prefix_k, prefix_v : device,
+ *          groups x sp tokens x kv_heads x dim (sp == 0: none, may be NULL); k, v : device,
+ *          batch x skv slots x kv_heads x dim. dim (64 or 128) is contiguous; the other
+ *          strides, in elements, are in `strides` (host pointer), each >= 0 and a multiple
+ *          of 8 (of a size of 1: anything), those of a key's or value's token at most 2^24;
+ *          no row of o meets another (as in quake_attention_window). All pointers 16-byte
+ *          aligned.
+ *   weight : device float, batch x kv_heads x skv, the slots contiguous, or NULL; its rows
+ *          lie apart. Slots from kv_len on are left as they are. o and weight overlap nothing.
+ *   prefix_lens, q_lens, kv_lens : device int32, one per group, sequence and sequence, or
+ *          NULL (sp, sq, skv): tokens they have in the padded buffers, clamped to 0 .. sp,
+ *          0 .. sq, 0 .. skv. Queries from q_len on are not read and their o is left as it
+ *          was; keys behind the lengths are not read.
+ *   workspace : device, 16-byte aligned, of the size
+ *          quake_attention_shared_workspace_size gives for these sizes, any content. Without
+ *          one (NULL) every sequence reads the prefix for itself; a weight needs one. It
+ *          lies outside the bytes from the first to the last of every operand. Calls that may
+ *          run at the same time need workspaces of their own.
+ *   batch a multiple of groups; batch, sq <= 2^24, sp + skv <= 2^30, heads <= 2^16, fewer
+ *   than 2^24 tiles of 32 rows of one key head (a row: one query of one head) and, with a
+ *   weight, of 128 slots of one key head; fewer than 2^30 rows of a group and key head; dtype
+ *   QUAKE_BF16 or QUAKE_F16 (else QUAKE_EDTYPE); t as in quake_attention. batch == 0 or
+ *   sq == 0 launches nothing.
+ * The same call gives the same bits every time (with a workspace others than without). A
+ * visible key or value that is not finite may spoil the outputs of other queries that share
+ * it, those that do not see it among them.
+ */
+typedef struct {
+  int64_t q[3], prefix_k[3], prefix_v[3], k[3], v[3], o[3]; /* batch (prefix: group), token, head */
+  int64_t weight[2];                                        /* batch, head */
+} quake_shared_strides;
+
+quake_status quake_attention_shared_workspace_size(int64_t batch, int64_t groups, int64_t sq,
+                                                   int64_t sp, int64_t skv, int64_t heads,
+                                                   int64_t kv_heads, int64_t dim, int weigh,
+                                                   int64_t* bytes);
+quake_status quake_attention_shared(const void* q, const void* prefix_k, const void* prefix_v,
+                                    const void* k, const void* v, void* o, float* weight,
+                                    const int32_t* prefix_lens, const int32_t* q_lens,
+                                    const int32_t* kv_lens, int64_t batch, int64_t groups,
+                                    int64_t sq, int64_t sp, int64_t skv, int64_t heads,
+                                    int64_t kv_heads, int64_t dim,
+                                    const quake_shared_strides* strides, quake_dtype dtype,
+                                    quake_mode mode, float t, void* workspace,
+                                    int64_t workspace_bytes, void* stream);
+
+/*
+ * quake_cache_evict — a key/value cache brought down to `budget` keys per key head by the
+ * weight they gathered (quake_attention_shared). Of a sequence with kv_len > budget each key
+ * head keeps the first `sinks` keys, the last `recent` ones, and of those between the
+ * budget - sinks - recent of largest weight (of equal ones the first; -0 is 0; NaN below
+ * all), in their order, in slots 0 .. budget - 1. Other sequences keep all.
+ *   k, v : device, batch x skv slots x kv_heads x dim of `dtype` (any; rows of 16 bytes or a
+ *          multiple, dim <= 4096); weight : device float, batch x kv_heads x skv; kv_lens :
+ *          device int32, one per sequence, clamped to 0 .. skv, or NULL (skv).
+ *   k_out, v_out, weight_out : the same with `slots` slots: k, v, weight themselves (slots ==
+ *          skv, same strides), the cache then shrinks in place, or another cache that meets
+ *          none of them. Slots behind the kept keys keep what they held in k_out and v_out,
+ *          and are 0 in weight_out, up to slot slots - 1.
+ *   lens_out : device int32, the kept keys of each sequence, min(kv_len, budget), or NULL;
+ *          may be kv_lens.
+ *   kept : device int32, batch x kv_heads x budget contiguous: the slots that the keys came
+ *          from, ascending, -1 behind the last. evicted : device int32, one per sequence:
+ *          max(kv_len - budget, 0), what a sequence's next position runs ahead of its cache.
+ *   strides : host pointer, in elements; of k, v and their outputs >= 0 and multiples of 16
+ *          bytes (of a size of 1: anything); dim and slots are contiguous. Rows of an output
+ *          lie apart, as o's in quake_attention_window; K and V may interleave. Pointers
+ *          16-byte aligned (weight and integers: 4). Apart from the above nothing that is
+ *          written meets anything.
+ *   1 <= budget <= slots, sinks + recent <= budget; skv, slots <= 2^30; batch x kv_heads <=
+ *   2^20. batch == 0 launches nothing.
+ */
+typedef struct {
+  int64_t k[3], v[3], k_out[3], v_out[3];  /* batch, slot, head */
+  int64_t weight[2], weight_out[2];        /* batch, head */
+} quake_evict_strides;
+
+quake_status quake_cache_evict(const void* k, const void* v, const float* weight,
+                               const int32_t* kv_lens, void* k_out, void* v_out,
+                               float* weight_out, int32_t* lens_out, int32_t* kept,
+                               int32_t* evicted, int64_t batch, int64_t skv, int64_t slots,
+                               int64_t kv_heads, int64_t dim, const quake_evict_strides* strides,
+                               int64_t budget, int64_t sinks, int64_t recent, quake_dtype dtype,
+                               void* stream);
 
 /*
  * quake_sample — the next token of every row of logits from one given random

@@ -27,7 +27,7 @@ C_CLIENT = os.path.join(ROOT, "tests", "c", "abi_smoke")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 SOURCES = ["elementwise.hip", "softmax.hip", "native16.hip", "gemm.hip", "attention.hip",
-           "window.hip", "sample.hip", "distill.hip", "ceiling.hip", "abi.cpp"]
+           "window.hip", "shared.hip", "evict.hip", "sample.hip", "distill.hip", "ceiling.hip", "abi.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [
@@ -40,7 +40,8 @@ FLAGS = [
 # Matrix-core accumulators in ordinary VGPRs: the attention kernels feed them
 # straight to VALU work, which cannot read the accumulation registers.
 EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 SHIFT64 = re.compile(r"\bv_(?:lshlrev_b64|lshrrev_b64|ashrrev_i64)\S* v\[\d+:\d+\], v(\d+),")

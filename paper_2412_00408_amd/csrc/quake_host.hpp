@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -66,6 +67,33 @@ inline bool meet(const void* a, int64_t na, const void* b, int64_t nb) {
 // Bytes from the first to behind the last of rows x cols elements, rows ld apart.
 inline int64_t rows_bytes(int64_t rows, int64_t cols, int64_t ld, int64_t elem) {
   return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * elem : 0;
+}
+
+// Whether no row of a tensor with n <= 4 outer dimensions shares elements with another:
+// in ascending order each stride reaches past what the smaller ones span. (Layouts that
+// interleave otherwise without meeting are refused as well; no view of a larger tensor by
+// slices and permutations is one.)
+inline bool rows_apart(const int64_t* stride, const int64_t* count, int n, int64_t row) {
+  int order[4] = {0, 1, 2, 3};
+  std::sort(order, order + n, [&](int a, int b) { return stride[a] < stride[b]; });
+  int64_t span = row;
+  for (int k = 0; k < n; ++k) {
+    const int i = order[k];
+    if (count[i] <= 1) continue;
+    if (stride[i] < span) return false;
+    span += stride[i] * (count[i] - 1);
+  }
+  return true;
+}
+// Bytes from the first to behind the last of count[0] x .. x count[n - 1] rows of `row`
+// elements of `elem` bytes.
+inline int64_t span_bytes(const int64_t* stride, const int64_t* count, int n, int64_t row, int64_t elem) {
+  int64_t last = row;
+  for (int i = 0; i < n; ++i) {
+    if (count[i] == 0) return 0;
+    last += count[i] > 1 ? stride[i] * (count[i] - 1) : 0;
+  }
+  return last * elem;
 }
 
 inline quake_status launch_status() {

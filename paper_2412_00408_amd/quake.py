@@ -54,12 +54,18 @@ def _load() -> ctypes.CDLL:
                                          ctypes.POINTER(ctypes.c_int64), i64, i64, ci, ci, cf, vp,
                                          i64, vp]
     L.quake_attention_window_workspace_size.argtypes = [i64] * 8 + [ctypes.POINTER(i64)]
+    L.quake_attention_shared.argtypes = [vp] * 6 + [fp, ip, ip, ip] + [i64] * 8 + [
+        ctypes.POINTER(ctypes.c_int64), ci, ci, cf, vp, i64, vp]
+    L.quake_attention_shared_workspace_size.argtypes = [i64] * 8 + [ci, ctypes.POINTER(i64)]
+    L.quake_cache_evict.argtypes = [vp, vp, fp, ip, vp, vp, fp, ip, ip, ip] + [i64] * 5 + [
+        ctypes.POINTER(ctypes.c_int64)] + [i64] * 3 + [ci, vp]
     L.quake_sample.argtypes = [vp, fp, ip, fp, i64, i64, i64, fp, ip, fp, fp, ci, ci, vp, i64, vp]
     L.quake_sample_workspace_size.argtypes = [i64, i64, ctypes.POINTER(i64)]
     L.quake_distill.argtypes = [vp, ip, vp, fp, fp, fp, vp] + [i64] * 7 + [ci, ci, ci, cf, vp, i64, vp]
     L.quake_distill_grad.argtypes = [vp, ip, vp, fp, fp, vp] + [i64] * 7 + [ci, ci, ci, cf, vp]
     L.quake_distill_workspace_size.argtypes = [i64, i64, ctypes.POINTER(i64)]
-    for f in (L.quake_attention_window, L.quake_attention_window_workspace_size, L.quake_sample,
+    for f in (L.quake_attention_shared, L.quake_attention_shared_workspace_size, L.quake_cache_evict,
+              L.quake_attention_window, L.quake_attention_window_workspace_size, L.quake_sample,
               L.quake_sample_workspace_size, L.quake_distill, L.quake_distill_grad,
               L.quake_distill_workspace_size, L.quake_exp, L.quake_exp16, L.quake_linear_gelu, L.quake_softmax, L.quake_gelu,
               L.quake_softmax_ws, L.quake_softmax_workspace_size, L.quake_softmax_noalloc,
@@ -339,6 +345,8 @@ def quake_softmax_causal(x, y=None, period=None, shift=0, mode=QUAKE_2, t=1.0, w
 # launches on the device of its first tensor, whichever is current.
 # ---------------------------------------------------------------------------
 _STRIDES = ctypes.c_int64 * 12
+_SHARED_STRIDES = ctypes.c_int64 * 20
+_EVICT_STRIDES = ctypes.c_int64 * 16
 _get_device = torch._C._cuda_getDevice
 
 
@@ -451,6 +459,151 @@ def quake_attention_window(q, k, v, o=None, window=2**31 - 1, sinks=0, q_lens=No
             DTYPES[dt], MODES[mode], 1.0 / dim ** 0.5 if t is None else t, ws, nbytes,
             _stream(q, stream))
     return o
+
+
+def attention_shared_workspace(q, k, prefix_k=None, weigh=False):
+    """A workspace for quake_attention_shared on tensors shaped like q, k and prefix_k, with
+    a weight or not, or None when that needs none. Any content; one per stream."""
+    b, sq, heads, dim = q.shape
+    groups, sp = (1, 0) if prefix_k is None else prefix_k.shape[:2]
+    return _new_workspace(_size("quake_attention_shared_workspace_size", b, groups, sq, sp, k.shape[1],
+                                heads, k.shape[2], dim, int(bool(weigh))), q.device)
+
+
+def quake_attention_shared(q, k, v, prefix_k=None, prefix_v=None, o=None, weight=None,
+                           prefix_lens=None, q_lens=None, kv_lens=None, mode=QUAKE_2, t=None,
+                           workspace=None, stream=None):
+    """Attention of the last q tokens of each sequence over a prefix that it shares with
+    others and over its own keys, query i seeing the whole prefix and its own keys
+    j <= pos_i: bfloat16 or float16 q [batch, sq, heads, dim], k, v [batch, skv, kv_heads,
+    dim] and prefix_k, prefix_v [groups, sp, kv_heads, dim] (or None), the batch being
+    `groups` runs of equally many sequences; dim 64 or 128 contiguous, other strides
+    multiples of 8; heads a multiple of kv_heads. prefix_lens [groups], q_lens, kv_lens
+    [batch]: int32, the tokens each has (default all); rows of o past q_lens keep what they
+    held (a new o: undefined). weight: float32 [batch, kv_heads, skv], to which each own key's
+    attention weight is added (see quake_cache_evict). t defaults to 1/sqrt(dim); |t q.k|
+    below 1e6. `workspace` (from attention_shared_workspace; apart from every operand):
+    without one each sequence reads the prefix for itself; a weight needs one."""
+    dev, dt = q.get_device(), q.dtype
+    for a, what in ((q, "q"), (k, "k"), (v, "v")):
+        _operand(a, what, dev)
+        if a.dim() != 4:
+            raise ValueError("%s needs [batch, tokens, heads, dim]" % what)
+    batch, sq, heads, dim = shape = q.shape
+    kvshape = k.shape
+    skv, kv_heads = kvshape[1], kvshape[2]
+    if k.dtype is not dt or v.dtype is not dt:
+        raise TypeError("q, k and v must have the same dtype")
+    if v.shape != kvshape or kvshape[0] != batch or kvshape[3] != dim:
+        raise ValueError("k and v must be [batch, skv, kv_heads, dim] with q's batch and dim")
+    if kv_heads == 0 or heads % kv_heads:
+        raise ValueError("heads must be a multiple of kv_heads")
+    groups = sp = 0
+    pk = pv = pks = pvs = None
+    if prefix_k is not None and prefix_v is not None:
+        for a, what in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+            _operand(a, what, dev, dt)
+        pshape = prefix_k.shape
+        if len(pshape) != 4 or prefix_v.shape != pshape or pshape[2:] != kvshape[2:]:
+            raise ValueError("prefix_k and prefix_v must be [groups, sp, kv_heads, dim]")
+        groups, sp = pshape[:2]
+        if groups == 0 or batch % groups:
+            raise ValueError("the batch must be a multiple of the prefix's groups")
+        pk, pv, pks, pvs = prefix_k.data_ptr(), prefix_v.data_ptr(), prefix_k.stride(), prefix_v.stride()
+        if pks[3] != 1 or pvs[3] != 1:
+            raise ValueError("prefix_k and prefix_v must have a contiguous last dimension")
+    elif prefix_k is not None or prefix_v is not None or prefix_lens is not None:
+        raise ValueError("a prefix needs prefix_k and prefix_v")
+    else:
+        groups, pks, pvs = 1, (0, 0, 0), (0, 0, 0)
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    if o is None:
+        o = torch.empty(shape, dtype=dt, device=q.device)
+    else:
+        _operand(o, "o", dev, dt, shape)
+        _apart(o, "o", ((q, "q"), (k, "k"), (v, "v"), (prefix_k, "prefix_k"), (prefix_v, "prefix_v"),
+                        (prefix_lens, "prefix_lens"), (q_lens, "q_lens"), (kv_lens, "kv_lens")))
+    os_ = o.stride()
+    if not qs[3] == ks[3] == vs[3] == os_[3] == 1:
+        raise ValueError("q, k, v and o must have a contiguous last dimension")
+    wp, ws_ = None, (0, 0)
+    if weight is not None:
+        ws_ = _weight_rows(weight, "weight", dev, (batch, kv_heads, skv))
+        wp = weight.data_ptr()
+        _apart(weight, "weight", ((o, "o"), (q, "q"), (k, "k"), (v, "v"), (prefix_k, "prefix_k"),
+                                  (prefix_v, "prefix_v"), (prefix_lens, "prefix_lens"),
+                                  (q_lens, "q_lens"), (kv_lens, "kv_lens")))
+        if workspace is None:
+            raise ValueError("a weight needs a workspace (attention_shared_workspace with weigh=True)")
+    pl = _per_row(prefix_lens, "prefix_lens", dev, groups, torch.int32)
+    ql = _per_row(q_lens, "q_lens", dev, batch, torch.int32)
+    kl = _per_row(kv_lens, "kv_lens", dev, batch, torch.int32)
+    ws, nbytes = _work(workspace, dev)
+    _launch("quake_attention_shared", dev, q.data_ptr(), pk, pv, k.data_ptr(), v.data_ptr(), o.data_ptr(),
+            wp, pl, ql, kl, batch, groups, sq, sp, skv, heads, kv_heads, dim,
+            _SHARED_STRIDES(*qs[:3], *pks[:3], *pvs[:3], *ks[:3], *vs[:3], *os_[:3], *ws_),
+            DTYPES[dt], MODES[mode], 1.0 / dim ** 0.5 if t is None else t, ws, nbytes, _stream(q, stream))
+    return o
+
+
+def _weight_rows(t, what, device, shape):
+    """Strides of the batch and the head of a weight."""
+    _operand(t, what, device, torch.float32, shape)
+    if t.stride(2) != 1 and shape[2] > 1:
+        raise ValueError("%s must have a contiguous last dimension" % what)
+    return t.stride()[:2]
+
+
+def quake_cache_evict(k, v, weight, budget, sinks=0, recent=0, kv_lens=None, out=None, kept=None,
+                      evicted=None, stream=None):
+    """Brings a cache k, v [batch, skv, kv_heads, dim] with the weight float32 [batch,
+    kv_heads, skv] that its keys gathered (quake_attention_shared) down to `budget` keys a key
+    head: the first `sinks`, the last `recent`, and of those between the ones of largest
+    weight (of equal ones the first), in their order. kv_lens: int32 [batch] (default skv
+    each); sequences within the budget keep all. In place, kv_lens too, or into `out`: (k, v,
+    weight) or (k, v, weight, kv_lens) of a cache of its own, with slots of its own number.
+    Weights behind the kept keys become 0; keys and values there keep what they held.
+    Returns (kept, evicted): int32 [batch, kv_heads, budget], the slots the keys came from, -1
+    behind the last, and int32 [batch], the keys that each sequence lost per head."""
+    dev, dt = k.get_device(), k.dtype
+    _operand(k, "k", dev)
+    if k.dim() != 4:
+        raise ValueError("k needs [batch, slots, heads, dim]")
+    batch, skv, kv_heads, dim = shape = k.shape
+    _operand(v, "v", dev, dt, shape)
+    wst = _weight_rows(weight, "weight", dev, (batch, kv_heads, skv))
+    kl = _per_row(kv_lens, "kv_lens", dev, batch, torch.int32)
+    if out is None:
+        ko, vo, wo, slots, lo = k, v, weight, skv, kl
+    else:
+        if len(out) not in (3, 4):
+            raise ValueError("out must be (k, v, weight) or (k, v, weight, kv_lens)")
+        ko, vo, wo = out[:3]
+        if ko.dim() != 4:
+            raise ValueError("out's k needs [batch, slots, heads, dim]")
+        slots = ko.shape[1]
+        for a, what in ((ko, "out's k"), (vo, "out's v")):
+            _operand(a, what, dev, dt, (batch, slots, kv_heads, dim))
+        lo = _per_row(out[3], "out's kv_lens", dev, batch, torch.int32) if len(out) == 4 else None
+    wost = _weight_rows(wo, "out's weight", dev, (batch, kv_heads, slots))
+    ks, vs, kos, vos = k.stride(), v.stride(), ko.stride(), vo.stride()
+    if dim > 1 and not ks[3] == vs[3] == kos[3] == vos[3] == 1:
+        raise ValueError("keys and values must have a contiguous last dimension")
+    if kept is None:
+        kept = torch.empty((batch, kv_heads, max(int(budget), 0)), dtype=torch.int32, device=k.device)
+    else:
+        _operand(kept, "kept", dev, torch.int32, (batch, kv_heads, budget))
+        if not kept.is_contiguous():
+            raise ValueError("kept must be contiguous")
+    if evicted is None:
+        evicted = torch.empty(batch, dtype=torch.int32, device=k.device)
+    else:
+        _per_row(evicted, "evicted", dev, batch, torch.int32)
+    _launch("quake_cache_evict", dev, k.data_ptr(), v.data_ptr(), weight.data_ptr(), kl, ko.data_ptr(),
+            vo.data_ptr(), wo.data_ptr(), lo, kept.data_ptr(), evicted.data_ptr(), batch, skv, slots,
+            kv_heads, dim, _EVICT_STRIDES(*ks[:3], *vs[:3], *kos[:3], *vos[:3], *wst, *wost), budget,
+            sinks, recent, DTYPES[dt], _stream(k, stream))
+    return kept, evicted
 
 
 def sample_workspace(x):
