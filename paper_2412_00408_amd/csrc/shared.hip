@@ -25,43 +25,83 @@ namespace qk {
 
 constexpr int kShWaves = 4;
 
+// A token's stride is below 2^24 + 1, so the strides that loops use are 32-bit ones.
 struct SharedArgs {
   const uint16_t *q, *pk, *pv, *k, *v;
   uint16_t* o;
   float* weight;                                // or null
   const int32_t *prefix_lens, *q_lens, *kv_lens;   // or null: sp, sq, skv
-  float2* stats;                                // of a row: M, 1 / sum of p; weight only
+  float2* stats;                                // of a row: M, 1 / sum of p (weights by rows)
   float* part;                                  // partial results, the groups' then the sequences'
+  float* scores;                                // or null; [row of a key head][slot] (weights by slots)
+  float* sums;                                  // parts of weights, by chunks of rows
   quake_shared_strides st;
+  int32_t pkt, pvt, kt, vt;                     // token strides
   int32_t groups, sq, sp, skv, group, kv_heads, members;
-  int32_t gtiles, gsplit, gmany;                // of a group's rows (gsplit 0: none) ..
-  int32_t tiles, nsplit, many;                  // .. and a sequence's: tiles of 32 rows, splits,
-                                                // whether 128 rows share a workgroup
-  uint32_t gwork;                               // workgroups of the groups' rows
+  int32_t gtiles, gmany, gchunk, gsplit;        // of a group's rows (gsplit 0: none) ..
+  int32_t tiles, many, chunk, nsplit;           // .. and a sequence's: tiles of 32 rows, whether 128
+                                                // rows share a workgroup, steps of 64 keys a
+                                                // workgroup takes, the most parts of a tile
+  uint32_t gwork, full, tail;                   // workgroups of groups' rows; a sequence's tiles that
+                                                // one workgroup takes, and those cut into parts
   float c0;                                     // 2^23 t / ln2 (EXACT: t / ln2)
 };
 
 // Partial results of a tile of 32 rows: M, sum, sum of p as it is, O.
 template <int D>
 constexpr int64_t kPart = 96 + 32 * D;
+constexpr int kShKeys = 64;                     // keys of a step
 
-__device__ __forceinline__ int64_t group_part(const SharedArgs& g, int64_t bh, int32_t tile) {
-  return (bh * g.gtiles + tile) * g.gsplit;     // first split's
-}
-__device__ __forceinline__ int64_t own_part(const SharedArgs& g, int64_t bh, int32_t tile, int64_t groups) {
-  return groups * g.kv_heads * g.gtiles * g.gsplit + (bh * g.tiles + tile) * g.nsplit;
-}
-
-// What a workgroup does: rows r0 on of a list, against a split of its keys.
+// What a workgroup does: rows r0 on of a list, against a part of its keys.
 struct Work {
   bool whole;               // the rows of a whole group, against its prefix alone
   int32_t b, hk;            // sequence (of a group: its first), key head
   int32_t r0, rows;         // first row, rows of the list
-  int32_t qlen, off;        // of the sequence; position of its query 0
+  int32_t off;              // position of the sequence's query 0
   int32_t plen, own;        // keys of the list: the prefix's, then the sequence's
-  int32_t split, nsplit;
-  int64_t part;             // of the workgroup's first 32 rows, split 0; -1: straight to o
+  int32_t n_lo, n_hi;       // blocks of 32 (128 rows: steps of 64) keys of the list
+  int64_t part;             // of the workgroup's first 32 rows; -1: straight to o
+  int32_t apart;            // parts from one tile's to the next one's
 };
+__device__ __forceinline__ int32_t list_blocks(int32_t plen, int32_t own, bool many) {
+  return many ? (plen + 63) / 64 + (own + 63) / 64 : (plen + 31) / 32 + (own + 31) / 32;
+}
+// parts that a list is cut into
+__device__ __forceinline__ int32_t list_parts(int32_t plen, int32_t own, bool many, int32_t chunk) {
+  const int32_t per = many ? chunk : 2 * chunk;
+  return (list_blocks(plen, own, many) + per - 1) / per;
+}
+// own keys that the rows of the tile at r0 see
+__device__ __forceinline__ int32_t tile_keys(const SharedArgs& g, int32_t off, int32_t r0, int32_t rows) {
+  return max(off + min(r0 + (g.many ? 32 * kShWaves : 32) - 1, rows - 1) / g.group + 1, 0);
+}
+__device__ __forceinline__ int32_t prefix_len(const SharedArgs& g, int32_t group) {
+  return g.sp == 0 ? 0 : seq_len(g.prefix_lens, group, g.sp);
+}
+// The first part of a tile: a group's; a sequence's, whose tiles are counted from the first
+// one that is cut.
+__device__ __forceinline__ int64_t group_part(const SharedArgs& g, int64_t bh, int32_t tile) {
+  return (bh * g.gtiles + tile) * g.gsplit;
+}
+__device__ __forceinline__ int64_t own_part(const SharedArgs& g, int64_t tile) {
+  return (int64_t)g.groups * g.kv_heads * g.gtiles * g.gsplit + tile * g.nsplit;
+}
+// tile number `id` of the sequences (in units of one workgroup's): sequence, key head, tile;
+// those that see most first
+struct TileOf {
+  uint32_t bh;
+  int32_t tile;
+};
+__device__ __forceinline__ TileOf tile_of(const SharedArgs& g, uint32_t id) {
+  const uint32_t tiles = g.many ? ((uint32_t)g.tiles + kShWaves - 1) / kShWaves : (uint32_t)g.tiles;
+  return {id / tiles, (int32_t)(tiles - 1u - id % tiles)};
+}
+// Workgroups go round the 8 XCDs: number `at` of n as each XCD takes consecutive ones, which
+// share most of their keys, for its own L2.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t at, uint32_t n) {
+  const uint32_t x = at & 7u, per = n >> 3, rest = n & 7u;
+  return x * per + min(x, rest) + (at >> 3);
+}
 struct RowOf {
   int32_t b, query, head, pos;
   bool live;
@@ -98,7 +138,7 @@ __device__ __forceinline__ void load_q(const SharedArgs& g, const RowOf& x, int 
 // swizzles). The last of the n keys stands for those behind it, whose probabilities
 // are 0.
 template <int D, bool IS_V, int ROWS>
-__device__ __forceinline__ void stage_run(uint32_t lds, const uint16_t* base, int64_t stride,
+__device__ __forceinline__ void stage_run(uint32_t lds, const uint16_t* base, int32_t stride,
                                           int32_t n0, int32_t n, int lane) {
   constexpr int CH = D / 8, RPL = 64 / CH, N = ROWS / RPL;   // chunks a row, rows a load, loads
   const int r = lane / CH, pc = lane % CH;
@@ -109,7 +149,7 @@ __device__ __forceinline__ void stage_run(uint32_t lds, const uint16_t* base, in
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int sw = IS_V ? vswizzle<D>(RPL * j + r) : kswizzle<D>(RPL * j + r);
-      lds_load16(lds + 1024 * j, row + 16u * (uint32_t)(pc ^ sw), b + (int64_t)2 * RPL * j * stride);
+      lds_load16(lds + 1024 * j, row + 16u * (uint32_t)(pc ^ sw), b + (int64_t)(2 * RPL * j) * stride);
     }
   } else {
 #pragma unroll
@@ -119,6 +159,9 @@ __device__ __forceinline__ void stage_run(uint32_t lds, const uint16_t* base, in
     }
   }
 }
+
+// slots of a row of scores
+__host__ __device__ constexpr int64_t score_row(int64_t skv) { return (skv + 31) / 32 * 32; }
 
 // -inf for the keys of the block from n0 on that lie behind key `lim`
 __device__ __forceinline__ void hide_behind(f32x16& s, int32_t n0, int32_t lim, int h) {
@@ -153,10 +196,10 @@ template <int D, bool IS_V, int ROWS>
 __device__ __forceinline__ void stage_list(uint32_t lds, const SharedArgs& g, const Work& w, const Lists& l,
                                            bool prefix, int32_t n0, int lane) {
   if (IS_V)
-    stage_run<D, true, ROWS>(lds, prefix ? l.pv : l.v, prefix ? g.st.prefix_v[1] : g.st.v[1], n0,
+    stage_run<D, true, ROWS>(lds, prefix ? l.pv : l.v, prefix ? g.pvt : g.vt, n0,
                              prefix ? w.plen : w.own, lane);
   else
-    stage_run<D, false, ROWS>(lds, prefix ? l.pk : l.k, prefix ? g.st.prefix_k[1] : g.st.k[1], n0,
+    stage_run<D, false, ROWS>(lds, prefix ? l.pk : l.k, prefix ? g.pkt : g.kt, n0,
                               prefix ? w.plen : w.own, lane);
 }
 
@@ -174,9 +217,11 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
   load_q<D>(g, x, h, qf);
   const Lists lists(g, w);
   const int32_t first = w.off + w.r0 / g.group;     // position of the first row
-  const int32_t pblocks = (w.plen + 31) >> 5, blocks = pblocks + ((w.own + 31) >> 5);
-  const int32_t n_lo = (int32_t)((int64_t)blocks * w.split / w.nsplit);
-  const int32_t n_hi = (int32_t)((int64_t)blocks * (w.split + 1) / w.nsplit);
+  const int32_t pblocks = (w.plen + 31) >> 5;
+  const int32_t n_lo = w.n_lo, n_hi = w.n_hi;
+  float* scores = nullptr;                          // of this lane's row, for the weights
+  if (WEIGH && g.scores != nullptr && !w.whole)
+    scores = g.scores + (((int64_t)w.b * g.kv_heads + w.hk) * (g.sq * g.group) + w.r0 + fr) * score_row(g.skv) + 4 * h;
   char* buf = s_buf + wave * kWave;
   const uint32_t lds = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf + wave * kWave);
@@ -198,9 +243,14 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     load_k(n_lo + wave);
     load_v(n_lo + wave);
   }
+  bool stored = false;
   for (int32_t n = n_lo + wave; n < n_hi; n += kShWaves) {
     const bool more = n + kShWaves < n_hi;
-    wait_loads<kLoads>();                           // K is here, V may be on its way
+    // K is here; the scores of the block before and V may be on their way
+    if (stored)
+      wait_loads<kLoads + 4>();
+    else
+      wait_loads<kLoads>();
     f32x16 s = {};
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) s = wmma<DT>(read_k<D>(buf, fr, h, ks), qf[ks], s);
@@ -209,6 +259,14 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     const bool p = n < pblocks;
     const int32_t n0 = 32 * (p ? n : n - pblocks);
     if (n0 + 31 > (p ? w.plen - 1 : first)) hide_behind(s, n0, p ? w.plen - 1 : x.pos, h);
+    if constexpr (WEIGH) {
+      stored = g.scores != nullptr && !p;
+      if (stored && x.live) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(scores + n0 + 8 * i) = float4{s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]};
+      }
+    }
     const float top = block_top<MODE>(s, g.c0);
     if (__any(top > acc.m + (kLift<DT> + kLazy))) {
       const int32_t e = raise_max<DT>(top, acc);
@@ -232,10 +290,13 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
       for (int r = 0; r < 16; r += 2)
         pr[r >> 3][(r >> 1) & 3] = prob_pair<DT, MODE>(s, r, g.c0, c1, acc.sum);
     }
-    if (more)
-      wait_loads<kLoads>();                         // V is here, the next K may be on its way
-    else
+    // V is here; the next K and the scores may be on their way
+    if (!more)
       wait_loads<0>();
+    else if (stored)
+      wait_loads<kLoads + 4>();
+    else
+      wait_loads<kLoads>();
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -288,7 +349,7 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
   }
   if (!x.live) return;
   if (w.part >= 0) {
-    float* to = g.part + (w.part + w.split) * kPart<D>;
+    float* to = g.part + w.part * kPart<D>;
     if (wave == 0 && h == 0) {
       to[fr] = m;
       to[32 + fr] = sum;
@@ -301,7 +362,7 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
   }
   if constexpr (WEIGH) {
     if (wave == 0 && h == 0)
-      g.stats[((int64_t)w.b * g.kv_heads + w.hk) * g.sq * g.group + w.r0 + fr] =
+      g.stats[((int64_t)w.b * g.kv_heads + w.hk) * 32 * g.tiles + w.r0 + fr] =
           every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -319,8 +380,6 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
 // 32; two tiles each of K and V), in the software pipeline of window_many_kernel: while
 // block n's scores become probabilities, the scores of block n + 1 and the second product
 // of block n - 1 are computed; one barrier a tile, between its blocks.
-constexpr int kShKeys = 64;
-
 template <int DT, int MODE, int D, bool WEIGH>
 __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, char* s_buf) {
   constexpr int kTile = 2 * kShKeys * D;            // bytes of K or V of a tile
@@ -332,9 +391,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   const int32_t first = w.off + min(w0, w.rows - 1) / g.group;
   const int32_t last = w.off + min(w0 + 31, w.rows - 1) / g.group;
   const int32_t ptiles = (w.plen + kShKeys - 1) / kShKeys;
-  const int32_t steps = ptiles + (w.own + kShKeys - 1) / kShKeys;
-  const int32_t n_lo = (int32_t)((int64_t)steps * w.split / w.nsplit);
-  const int32_t n_hi = (int32_t)((int64_t)steps * (w.split + 1) / w.nsplit);
+  const int32_t n_lo = w.n_lo, n_hi = w.n_hi;
   // tiles of which this wave's rows may see something
   const int32_t seen = w.whole || last < 0 ? 0 : last / kShKeys + 1;
   const int32_t t_hi = __any(x.live) ? min(n_hi, ptiles + seen) : n_lo;
@@ -479,7 +536,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   if constexpr (WEIGH) all += other_half(all);
   if (w.part >= 0) {
     if (!x.live) return;
-    float* to = g.part + (w.part + (int64_t)wave * w.nsplit + w.split) * kPart<D>;
+    float* to = g.part + (w.part + (int64_t)wave * w.apart) * kPart<D>;
     if (h == 0) {
       to[fr] = acc.m;
       to[32 + fr] = sum;
@@ -495,7 +552,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   }
   if constexpr (WEIGH) {
     if (h == 0 && x.live)
-      g.stats[((int64_t)w.b * g.kv_heads + w.hk) * g.sq * g.group + w0 + fr] =
+      g.stats[((int64_t)w.b * g.kv_heads + w.hk) * 32 * g.tiles + w0 + fr] =
           all > 0.0f ? float2{acc.m, 1.0f / all} : float2{0.0f, 0.0f};
   }
   // Rows of the output through LDS (the wave's own rows, chunks swizzled as K's), so
@@ -525,70 +582,118 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
 }
 
 // The groups' rows against the prefixes, then each sequence's against its own keys (where no
-// rows of groups are formed: against the prefix, too). Workgroups go round the 8 XCDs: each
-// gets consecutive ones of either kind, which share most of their keys, for its own L2.
+// rows of groups are formed: against the prefix first), the tiles that one workgroup takes
+// before those that are cut into parts.
 template <int DT, int MODE, int D, bool WEIGH>
 __global__ __launch_bounds__(64 * kShWaves, 2) void shared_kernel(SharedArgs g) {
   __shared__ __attribute__((aligned(16))) char s_buf[4 * 2 * kShKeys * D];
   __shared__ float s_row[3 * kShWaves * 32];
-  const bool whole = blockIdx.x < g.gwork;
-  const uint32_t at = whole ? blockIdx.x : blockIdx.x - g.gwork, work = whole ? g.gwork : gridDim.x - g.gwork;
-  const uint32_t c = at & 7u, per = work >> 3, rest = work & 7u;
-  uint32_t id = c * per + min(c, rest) + (at >> 3);
   Work w;
-  w.whole = whole;
-  const bool many = (whole ? g.gmany : g.many) != 0;
-  const uint32_t tiles = ((uint32_t)(whole ? g.gtiles : g.tiles) + (many ? kShWaves - 1 : 0)) / (many ? kShWaves : 1);
-  w.nsplit = whole ? g.gsplit : g.nsplit;
-  const uint32_t tile = id % tiles;
-  id /= tiles;
-  w.split = (int32_t)(id % (uint32_t)w.nsplit);
-  const uint32_t bh = id / (uint32_t)w.nsplit;
-  w.hk = (int32_t)(bh % (uint32_t)g.kv_heads);
-  w.b = (int32_t)(bh / (uint32_t)g.kv_heads) * (whole ? g.members : 1);
-  const int32_t t32 = (int32_t)tile * (many ? kShWaves : 1);
-  w.r0 = 32 * t32;
-  const int32_t grp = w.b / g.members;
-  const int32_t plen = g.sp == 0 ? 0 : seq_len(g.prefix_lens, grp, g.sp);
-  if (whole) {
-    w.qlen = w.off = w.own = 0;
+  bool many;
+  int32_t split = 0;
+  if (blockIdx.x < g.gwork) {
+    w.whole = true;
+    many = g.gmany != 0;
+    const uint32_t tiles = many ? ((uint32_t)g.gtiles + kShWaves - 1) / kShWaves : (uint32_t)g.gtiles;
+    uint32_t id = by_xcd(blockIdx.x, g.gwork);
+    const int32_t t32 = (int32_t)(id % tiles) * (many ? kShWaves : 1);
+    id /= tiles;
+    split = (int32_t)(id % (uint32_t)g.gsplit);
+    const uint32_t bh = id / (uint32_t)g.gsplit;
+    w.hk = (int32_t)(bh % (uint32_t)g.kv_heads);
+    w.b = (int32_t)(bh / (uint32_t)g.kv_heads) * g.members;
+    w.r0 = 32 * t32;
     w.rows = g.members * g.sq * g.group;
-    w.plen = plen;
-    w.part = group_part(g, bh, t32);
+    w.off = w.own = 0;
+    w.plen = prefix_len(g, w.b / g.members);
+    w.apart = g.gsplit;
+    w.part = group_part(g, bh, t32) + split;
   } else {
-    w.qlen = seq_len(g.q_lens, w.b, g.sq);
-    w.off = seq_len(g.kv_lens, w.b, g.skv) - w.qlen;
-    w.rows = w.qlen * g.group;
-    const int32_t last = w.off + min(w.r0 + (many ? 32 * kShWaves : 32) - 1, w.rows - 1) / g.group;
-    w.own = max(last + 1, 0);
-    w.plen = g.gsplit > 0 ? 0 : plen;
-    w.part = g.gsplit == 0 && g.nsplit == 1 ? -1 : own_part(g, bh, t32, g.groups);
+    w.whole = false;
+    many = g.many != 0;
+    const uint32_t at = blockIdx.x - g.gwork;
+    uint32_t id;
+    w.part = -1;
+    w.apart = g.nsplit;
+    if (at < g.full) {
+      id = by_xcd(at, g.full);
+    } else {
+      const uint32_t cut = by_xcd(at - g.full, g.tail * (uint32_t)g.nsplit);
+      split = (int32_t)(cut % (uint32_t)g.nsplit);
+      id = cut / (uint32_t)g.nsplit;
+      w.part = own_part(g, (int64_t)id * (many ? kShWaves : 1)) + split;
+      id += g.full;
+    }
+    const TileOf t = tile_of(g, id);
+    w.hk = (int32_t)(t.bh % (uint32_t)g.kv_heads);
+    w.b = (int32_t)(t.bh / (uint32_t)g.kv_heads);
+    w.r0 = t.tile * (many ? 32 * kShWaves : 32);
+    const int32_t qlen = seq_len(g.q_lens, w.b, g.sq);
+    w.off = seq_len(g.kv_lens, w.b, g.skv) - qlen;
+    w.rows = qlen * g.group;
+    w.own = tile_keys(g, w.off, w.r0, w.rows);
+    w.plen = g.gsplit > 0 ? 0 : prefix_len(g, w.b / g.members);
   }
   if (w.r0 >= w.rows) return;
+  w.n_lo = 0;
+  w.n_hi = list_blocks(w.plen, w.own, many);
+  if (w.part >= 0) {
+    const int32_t per = (w.whole ? g.gchunk : g.chunk) * (many ? 1 : 2);
+    w.n_lo = split * per;
+    w.n_hi = min(w.n_hi, w.n_lo + per);
+    if (w.n_lo >= w.n_hi) return;
+  }
   if (many)
     many_rows<DT, MODE, D, WEIGH>(g, w, s_buf);
   else
     few_rows<DT, MODE, D, WEIGH>(g, w, s_buf, s_row);
 }
 
-// Joins a row's partial results, the group's and the sequence's, a lane for every four dims:
-// D / 4 lanes, which take the results one after the other, or (WIDE) the whole workgroup,
-// whose 1024 / D such teams take every so many-th. Several loads are in flight; the order
+// The parts of a row: first those of the group's tile, then those of the sequence's.
+struct Parts {
+  const float *pg, *po;      // first parts
+  int32_t ng, n;             // the group's, all
+  int32_t fg, fo;            // the row in either tile
+};
+template <int D>
+__device__ __forceinline__ Parts parts_of(const SharedArgs& g, uint32_t id, uint32_t bh, int b, int32_t row,
+                                          int32_t rows, int32_t off) {
+  Parts p;
+  const int hk = bh % (uint32_t)g.kv_heads, grp = b / g.members;
+  const int32_t plen = prefix_len(g, grp);
+  const int32_t of_group = (b - grp * g.members) * g.sq * g.group + row;
+  const int wide = g.many ? kShWaves : 1;
+  const int32_t t32 = row >> 5;
+  p.ng = g.gsplit > 0 ? list_parts(plen, 0, g.gmany != 0, g.gchunk) : 0;
+  p.pg = g.part + group_part(g, (int64_t)grp * g.kv_heads + hk, of_group >> 5) * kPart<D>;
+  p.po = g.part + own_part(g, (int64_t)(id - g.full) * wide + t32 % wide) * kPart<D>;
+  p.n = p.ng + list_parts(g.gsplit > 0 ? 0 : plen, tile_keys(g, off, t32 / wide * wide * 32, rows), g.many != 0, g.chunk);
+  p.fg = of_group & 31;
+  p.fo = row & 31;
+  return p;
+}
+template <int D>
+__device__ __forceinline__ const float* part_at(const Parts& p, int32_t i, int32_t& fr) {
+  fr = i < p.ng ? p.fg : p.fo;
+  return i < p.ng ? p.pg + (int64_t)i * kPart<D> : p.po + (int64_t)(i - p.ng) * kPart<D>;
+}
+
+// Joins the parts of a row: T teams of D / 4 lanes, a lane for every four dims, which take
+// every T-th part with several loads in flight; then the teams' results in LDS. The order
 // is fixed.
-template <int DT, int D, bool WEIGH, bool WIDE>
-__global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs g) {
-  constexpr int C = D / 4, SL = WIDE ? 256 / C : 1, U = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t id = WIDE ? blockIdx.x : blockIdx.x * (256u / C) + threadIdx.x / C;   // of all rows
-  const uint32_t item = id >> 5, bh = item / (uint32_t)g.tiles;
-  const int32_t row = 32 * (int32_t)(item % (uint32_t)g.tiles) + (int32_t)(id & 31u);
-  const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
-  if (b >= g.members * g.groups || row >= seq_len(g.q_lens, b, g.sq) * g.group) return;
-  const int grp = b / g.members;
-  const int32_t of_group = (b - grp * g.members) * g.sq * g.group + row;   // among the group's rows
-  const float* pg = g.part + group_part(g, (int64_t)grp * g.kv_heads + hk, of_group >> 5) * kPart<D>;
-  const float* po = g.part + own_part(g, bh, row >> 5, g.groups) * kPart<D>;
-  const int c = lane % C, total = g.gsplit + g.nsplit;
+template <int DT, int D, bool WEIGH, int T>
+__device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, float* s_row, float4 (*s_v)[D / 4]) {
+  constexpr int C = D / 4, TEAMS = 256 / C, R = TEAMS / T, U = 4;
+  const int team = threadIdx.x / C, c = threadIdx.x % C, k = team % T;   // team k of its row
+  const uint32_t n = block * R + team / T;                               // row of all that are joined
+  const uint32_t per = g.many ? 32 * kShWaves : 32;
+  const uint32_t id = g.full + n / per;
+  const TileOf t = tile_of(g, id);
+  const int b = (int)(t.bh / (uint32_t)g.kv_heads), hk = (int)(t.bh % (uint32_t)g.kv_heads);
+  const int32_t row = t.tile * (int32_t)per + (int32_t)(n % per);
+  const bool in = n / per < g.tail;
+  const int32_t qlen = in ? seq_len(g.q_lens, b, g.sq) : 0, rows = qlen * g.group;
+  const bool live = row < rows;
   float m = kNoMax, sum = 0.0f, every = 0.0f;
   float4 v{0.0f, 0.0f, 0.0f, 0.0f};
   auto add = [&](float om, float os, float oe, float4 ov) {
@@ -602,47 +707,42 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs g) {
     v = float4{two(v.x, ov.x), two(v.y, ov.y), two(v.z, ov.z), two(v.w, ov.w)};
     m = top;
   };
-  for (int s0 = WIDE ? threadIdx.x / C : 0; s0 < total; s0 += U * SL) {
-    float om[U], os[U], oe[U];
-    float4 ov[U];
+  if (live) {
+    const Parts p = parts_of<D>(g, id, t.bh, b, row, rows, seq_len(g.kv_lens, b, g.skv) - qlen);
+    for (int32_t s0 = k; s0 < p.n; s0 += U * T) {
+      float om[U], os[U], oe[U];
+      float4 ov[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) {   // past the last one: that one again, not added
-      const int i = min(s0 + j * SL, total - 1);
-      const bool own = i >= g.gsplit;
-      const float* p = own ? po + (i - g.gsplit) * kPart<D> : pg + i * kPart<D>;
-      const int fr = (own ? row : of_group) & 31;
-      om[j] = p[fr];
-      os[j] = p[32 + fr];
-      oe[j] = WEIGH ? p[64 + fr] : 0.0f;
-      ov[j] = *reinterpret_cast<const float4*>(p + 96 + fr * D + 4 * c);
+      for (int j = 0; j < U; ++j) {   // past the last one: that one again, not added
+        int32_t fr;
+        const float* x = part_at<D>(p, min(s0 + j * T, p.n - 1), fr);
+        om[j] = x[fr];
+        os[j] = x[32 + fr];
+        oe[j] = WEIGH ? x[64 + fr] : 0.0f;
+        ov[j] = *reinterpret_cast<const float4*>(x + 96 + fr * D + 4 * c);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (s0 + j * T < p.n) add(om[j], os[j], oe[j], ov[j]);
     }
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (s0 + j * SL < total) add(om[j], os[j], oe[j], ov[j]);
   }
-  if constexpr (WIDE) {
-    constexpr int W = 4;
-#pragma unroll
-    for (int o = C; o < 64; o <<= 1)
-      add(__shfl_xor(m, o, 64), __shfl_xor(sum, o, 64), __shfl_xor(every, o, 64),
-          float4{__shfl_xor(v.x, o, 64), __shfl_xor(v.y, o, 64), __shfl_xor(v.z, o, 64),
-                 __shfl_xor(v.w, o, 64)});
-    __shared__ float s_m[W], s_sum[W], s_all[W];
-    __shared__ float4 s_v[W][C];
-    if (lane < C) s_v[wave][c] = v;
-    if (lane == 0) {
-      s_m[wave] = m;
-      s_sum[wave] = sum;
-      s_all[wave] = every;
+  if constexpr (T > 1) {
+    s_v[team][c] = v;
+    if (c == 0) {
+      s_row[team] = m;
+      s_row[TEAMS + team] = sum;
+      s_row[2 * TEAMS + team] = every;
     }
     __syncthreads();
-    if (wave > 0 || lane >= C) return;
+    if (k > 0) return;
 #pragma unroll
-    for (int o = 1; o < W; ++o) add(s_m[o], s_sum[o], s_all[o], s_v[o][c]);
+    for (int o = 1; o < T; ++o)
+      add(s_row[team + o], s_row[TEAMS + team + o], s_row[2 * TEAMS + team + o], s_v[team + o][c]);
   }
+  if (!live) return;
   if constexpr (WEIGH) {
-    if (c == 0)
-      g.stats[(int64_t)bh * g.sq * g.group + row] = every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
+    if (c == 0 && g.scores == nullptr)
+      g.stats[(int64_t)t.bh * 32 * g.tiles + row] = every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   uint16_t* orow = g.o + b * g.st.o[0] + (row / g.group) * g.st.o[1] + (hk * g.group + row % g.group) * g.st.o[2];
@@ -650,44 +750,152 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs g) {
       u32x2{wpack<DT>(v.x * inv, v.y * inv), wpack<DT>(v.z * inv, v.w * inv)};
 }
 
-// The weight that 128 slots gather, 32 a wave, which holds their K and goes over the rows
-// that see them: the scores again, the exponentials against the row's final M, times
-// 1 / sum. Each slot has one wave and a fixed order of rows.
-constexpr int kWeighSlots = 32 * kShWaves;
+// The weight of kWeighSlots slots of a key head whose rows are one tile of 32: the scores
+// that the tiles left, against the rows' final M, which is joined here from the parts.
+constexpr int kScoreSlots = 1024;
+
+template <int MODE, int D>
+__device__ __forceinline__ void weigh_slots(const SharedArgs& g, uint32_t bh, int32_t j0, float* s_row) {
+  const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)(bh % (uint32_t)g.kv_heads);
+  const int32_t qlen = seq_len(g.q_lens, b, g.sq), kvlen = seq_len(g.kv_lens, b, g.skv);
+  const int32_t rows = qlen * g.group, off = kvlen - qlen;
+  if (j0 >= kvlen || rows == 0) return;
+  {
+    // 8 lanes a row
+    const int32_t row = threadIdx.x >> 3, k = threadIdx.x & 7;
+    float m = kNoMax, all = 0.0f;
+    if (row < rows) {
+      const Parts p = parts_of<D>(g, bh, bh, b, row, rows, off);
+      for (int32_t i = k; i < p.n; i += 8) {
+        int32_t fr;
+        const float* x = part_at<D>(p, i, fr);
+        const float top = fmaxf(m, x[fr]);
+        all = __builtin_amdgcn_ldexpf(all, down_shift(m, top)) +
+              __builtin_amdgcn_ldexpf(x[64 + fr], down_shift(x[fr], top));
+        m = top;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      const float om = __shfl_xor(m, o, 64), oa = __shfl_xor(all, o, 64), top = fmaxf(m, om);
+      all = __builtin_amdgcn_ldexpf(all, down_shift(m, top)) + __builtin_amdgcn_ldexpf(oa, down_shift(om, top));
+      m = top;
+    }
+    if (k == 0) {
+      s_row[row] = all > 0.0f ? row_c1<MODE>(m) : 0.0f;
+      s_row[32 + row] = all > 0.0f ? 1.0f / all : 0.0f;
+    }
+  }
+  __syncthreads();
+  const int32_t j = j0 + 4 * (int32_t)threadIdx.x;
+  if (j >= kvlen) return;
+  const int64_t ld = score_row(g.skv);
+  const float* x = g.scores + (int64_t)bh * (g.sq * g.group) * ld + j;
+  float a[4] = {};
+  for (int32_t r = 0; r < rows; ++r) {
+    if (off + r / g.group < j) continue;            // no part of this row's tile need be there
+    const float4 s = *reinterpret_cast<const float4*>(x + r * ld);
+    const float c1 = s_row[r], inv = s_row[32 + r];
+    a[0] = __builtin_fmaf(qexp_row<MODE, true>(s.x, g.c0, c1), inv, a[0]);
+    a[1] = __builtin_fmaf(qexp_row<MODE, true>(s.y, g.c0, c1), inv, a[1]);
+    a[2] = __builtin_fmaf(qexp_row<MODE, true>(s.z, g.c0, c1), inv, a[2]);
+    a[3] = __builtin_fmaf(qexp_row<MODE, true>(s.w, g.c0, c1), inv, a[3]);
+  }
+  float* to = g.weight + b * g.st.weight[0] + hk * g.st.weight[1] + j;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (j + i < kvlen) to[i] += a[i];
+}
+
+// Joins the parts of the rows and, in workgroups of their own, weighs the slots.
+template <int DT, int MODE, int D, bool WEIGH, int T>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs g, uint32_t joins, uint32_t slot_blocks) {
+  __shared__ float s_row[3 * 32];
+  __shared__ float4 s_v[1024 / D][D / 4];
+  if constexpr (WEIGH) {
+    if (blockIdx.x >= joins) {
+      const uint32_t i = blockIdx.x - joins;
+      weigh_slots<MODE, D>(g, i / slot_blocks, (int32_t)(i % slot_blocks) * kScoreSlots, s_row);
+      return;
+    }
+  }
+  join_rows<DT, D, WEIGH, T>(g, blockIdx.x, s_row, s_v);
+}
+
+// The weight that 128 slots gather from a chunk of the rows. A wave holds the K of 32 slots;
+// the rows' queries go through LDS, 64 at a time for all waves, two buffers: the scores
+// again, the exponentials against the rows' final M, times 1 / sum. A slot's rows are added
+// in a fixed order, chunks by weigh_add_kernel.
+constexpr int kWeighSlots = 32 * kShWaves, kWeighStep = 64, kWeighRows = 2048;
 
 template <int DT, int MODE, int D>
-__global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs g, uint32_t slot_tiles) {
+__global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs g, uint32_t slot_tiles,
+                                                                      uint32_t chunks) {
+  constexpr int kBuf = 2 * kWeighStep * D + 1024;    // bytes: queries, then M and 1 / sum of 128 rows
+  constexpr int CH = D / 8, RPL = 64 / CH, kRows = kWeighStep / kShWaves, N = kRows / RPL;
+  __shared__ __attribute__((aligned(16))) char s_buf[2 * kBuf];
   const int lane = threadIdx.x & 63, fr = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t bh = blockIdx.x / slot_tiles;
+  const uint32_t chunk = blockIdx.x % chunks, item = blockIdx.x / chunks;
+  const uint32_t bh = item / slot_tiles;
   const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
   const int32_t qlen = seq_len(g.q_lens, b, g.sq), kvlen = seq_len(g.kv_lens, b, g.skv);
-  const int32_t j0 = (int32_t)(blockIdx.x % slot_tiles) * kWeighSlots + 32 * wave;
-  if (j0 >= kvlen) return;
+  const int32_t first_slot = (int32_t)(item % slot_tiles) * kWeighSlots, j0 = first_slot + 32 * wave;
+  if (first_slot >= kvlen) return;
+  const int32_t off = kvlen - qlen, rows = qlen * g.group;
+  // rows of this chunk that may see the first slot
+  const int32_t from = max(0, first_slot - off);
+  const int32_t lo = max(from >= qlen ? rows : (from * g.group) & ~(kWeighStep - 1), (int32_t)chunk * kWeighRows);
+  const int32_t hi = min(rows, ((int32_t)chunk + 1) * kWeighRows);
+
   u32x4 kf[D / 16];
   {
-    const uint16_t* kr = g.k + b * g.st.k[0] + min(j0 + fr, kvlen - 1) * g.st.k[1] + hk * g.st.k[2] + 8 * h;
+    const uint16_t* kr = g.k + b * g.st.k[0] + (int64_t)min(j0 + fr, kvlen - 1) * g.kt + hk * g.st.k[2] + 8 * h;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) kf[ks] = *reinterpret_cast<const u32x4*>(kr + 16 * ks);
   }
-  const int32_t off = kvlen - qlen, rows = qlen * g.group;
-  const int32_t from = max(0, j0 - off);             // the first query that sees slot j0
-  const float2* stats = g.stats + (int64_t)bh * g.sq * g.group;
+  settle(kf);
+  const uint16_t* Q = g.q + b * g.st.q[0] + hk * g.group * g.st.q[2];
+  const float2* stats = g.stats + (int64_t)bh * 32 * g.tiles;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf);
+  // queries r0 on to buffer `at`: this wave's kRows of them, chunks swizzled as K's
+  auto load = [&](int32_t r0, int at) {
+    uint32_t lds = lds0 + kBuf * at;
+    asm volatile("" : "+s"(lds));
+    const int r = lane / CH, pc = lane % CH;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int in = kRows * wave + RPL * j + r;
+      const int32_t row = min(r0 + in, rows - 1);
+      const uint16_t* p = Q + (row / g.group) * g.st.q[1] + (row % g.group) * g.st.q[2];
+      lds_load16(lds + kRows * 2 * D * wave + 1024 * j, p + 8 * (pc ^ kswizzle<D>(RPL * j + r)));
+    }
+    if (wave == 0) lds_load16(lds + 2 * kWeighStep * D, reinterpret_cast<const char*>(stats + r0) + 16 * lane);
+  };
   float acc[16] = {};
-  for (int32_t r0 = from >= qlen ? rows : from * g.group & ~31; r0 < rows; r0 += 32) {
-    const int32_t row = min(r0 + fr, rows - 1);
-    const int32_t query = row / g.group, head = hk * g.group + row % g.group;
-    const uint16_t* qr = g.q + b * g.st.q[0] + query * g.st.q[1] + head * g.st.q[2] + 8 * h;
-    f32x16 s = {};
+  if (lo < hi) load(lo, 0);
+  int at = 0;
+  for (int32_t r0 = lo; r0 < hi; r0 += kWeighStep, at ^= 1) {
+    wait_loads<0>();
+    __syncthreads();                                 // this buffer is here, the other one done with
+    if (r0 + kWeighStep < hi) load(r0 + kWeighStep, at ^ 1);
+    const char* buf = s_buf + kBuf * at;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      s = wmma<DT>(kf[ks], *reinterpret_cast<const u32x4*>(qr + 16 * ks), s);
-    if (off + r0 / g.group < j0 + 31) hide_behind(s, j0, off + query, h);
-    const float2 ms = stats[row];
-    const float c1 = row_c1<MODE>(ms.x), inv = r0 + fr < rows ? ms.y : 0.0f;
+    for (int t = 0; t < kWeighStep / 32; ++t) {
+      const int32_t row = r0 + 32 * t + fr;
+      f32x16 s = {};
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      acc[r] = __builtin_fmaf(qexp_row<MODE, true>(s[r], g.c0, c1), inv, acc[r]);
+      for (int ks = 0; ks < D / 16; ++ks)
+        s = wmma<DT>(kf[ks], read_k<D>(buf + 64 * D * t, fr, h, ks), s);
+      const float2 ms = *reinterpret_cast<const float2*>(buf + 2 * kWeighStep * D + 8 * (32 * t + fr));
+      const bool in = row < hi;
+      const float c1 = in ? row_c1<MODE>(ms.x) : -INFINITY, inv = in ? ms.y : 0.0f;   // e = 0 behind the rows
+      if (off + (r0 + 32 * t) / g.group < j0 + 31) hide_behind(s, j0, off + row / g.group, h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        acc[r] = __builtin_fmaf(qexp_row<MODE, true>(s[r], g.c0, c1), inv, acc[r]);
+    }
   }
   float mine = 0.0f;                                 // lane r < 16 of a half: slot r's sum
 #pragma unroll
@@ -698,7 +906,24 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
     mine = fr == r ? v : mine;
   }
   const int32_t j = j0 + 8 * (fr >> 2) + 4 * h + (fr & 3);
-  if (fr < 16 && j < kvlen) g.weight[b * g.st.weight[0] + hk * g.st.weight[1] + j] += mine;
+  if (fr >= 16 || j >= kvlen) return;
+  if (chunks == 1)
+    g.weight[b * g.st.weight[0] + hk * g.st.weight[1] + j] += mine;
+  else
+    g.sums[((int64_t)bh * chunks + chunk) * g.skv + j] = mine;
+}
+
+__global__ __launch_bounds__(256) void weigh_add_kernel(SharedArgs g, uint32_t blocks, uint32_t chunks) {
+  const uint32_t bh = blockIdx.x / blocks;
+  const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
+  const int32_t kvlen = seq_len(g.kv_lens, b, g.skv), qlen = seq_len(g.q_lens, b, g.sq);
+  const int32_t j = (int32_t)(blockIdx.x % blocks) * 256 + (int32_t)threadIdx.x;
+  if (j >= kvlen) return;
+  const float* x = g.sums + (int64_t)bh * chunks * g.skv + j;
+  const uint32_t n = ((uint32_t)(qlen * g.group) + kWeighRows - 1) / kWeighRows;
+  float v = 0.0f;
+  for (uint32_t i = 0; i < n; ++i) v += x[(int64_t)i * g.skv];
+  g.weight[b * g.st.weight[0] + hk * g.st.weight[1] + j] += v;
 }
 
 // ---------------------------------------------------------------------------
@@ -721,72 +946,110 @@ static bool shared_shape_ok(const SharedShape& s) {
   // workgroups of 256 threads: a launch takes fewer than 2^32 threads
   return s.batch * s.kv_heads < (1 << 24) && s.batch * s.kv_heads * s.tiles() < (1 << 24);
 }
-static int64_t slot_tiles(const SharedShape& s) { return (s.skv + kWeighSlots - 1) / kWeighSlots; }
-static bool weigh_shape_ok(const SharedShape& s) {
-  return s.batch * s.kv_heads * slot_tiles(s) < (1 << 24);
-}
-static int64_t stats_bytes(const SharedShape& s) {
-  return (s.batch * s.heads * s.sq * 8 + 15) / 16 * 16;
-}
-
 // How a call is cut up. Rows of a whole group against the prefix where a sequence alone has
 // few: the prefix is then read once for all, and its scores are full tiles.
 struct SharedPlan {
-  int64_t gtiles = 0, gsplit = 0, tiles = 0, nsplit = 1;
-  bool gmany = false, many = false;
-  bool join() const { return gsplit > 0 || nsplit > 1; }
+  int64_t gtiles = 0, gchunk = 1, gsplit = 0, gitems = 0;   // items: tiles of a workgroup
+  int64_t tiles = 0, chunk = 1, nsplit = 1, full = 0, tail = 0;
+  bool gmany = false, many = false, stored = false;
 };
-constexpr int64_t kShTarget = 512, kShSplitKeys = 128, kShSplitFrom = 512;
-constexpr int64_t kShJoinFew = 8;
+constexpr int64_t kShSlots = 512;       // workgroups that run at once
+constexpr int64_t kManyRows = 96;
 
-static SharedPlan shared_plan(const SharedShape& s) {
+static int64_t wide_tiles(int64_t rows, bool many) { return many ? (rows + 127) / 128 : (rows + 31) / 32; }
+
+static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) {
   SharedPlan p;
   const int64_t rows = s.sq * s.group(), all = rows * (s.batch / s.groups);
-  const auto wide = [](int64_t n, bool many) { return many ? (n + 127) / 128 : (n + 31) / 32; };
-  const auto splits = [&](int64_t items, int64_t keys) {
-    return items == 0 || keys < kShSplitFrom ? 1
-                                             : std::max<int64_t>(1, std::min(keys / kShSplitKeys, kShTarget / items));
-  };
   p.tiles = (rows + 31) / 32;
-  p.many = rows >= 96;
-  int64_t own = s.skv;
-  if (s.sp > 0 && rows < 96 && all > rows) {
+  p.many = rows >= kManyRows;
+  const int64_t items = s.batch * s.kv_heads * wide_tiles(rows, p.many);
+  p.full = items;
+  if (!workspace || items == 0 || items >= (1 << 18)) return p;   // 32 rows a tile are joined in one launch
+  p.stored = weigh && rows <= 32;
+  const int64_t psteps = (s.sp + 63) / 64;
+  int64_t steps = (s.skv + 63) / 64;
+  if (s.sp > 0 && rows < kManyRows && all > rows) {
     p.gtiles = (all + 31) / 32;
     p.gmany = all > 32;
-    p.gsplit = splits(s.groups * s.kv_heads * wide(all, p.gmany), s.sp);
+    p.gitems = s.groups * s.kv_heads * wide_tiles(all, p.gmany);
+    p.gchunk = std::max<int64_t>(getenv("GMIN") ? atoi(getenv("GMIN")) : 4, (psteps * p.gitems + (getenv("GN") ? atoi(getenv("GN")) : kShSlots) - 1) / (getenv("GN") ? atoi(getenv("GN")) : kShSlots));
+    p.gsplit = (psteps + p.gchunk - 1) / p.gchunk;
   } else {
-    own += s.sp;
+    steps += psteps;
   }
-  p.nsplit = splits(s.batch * s.kv_heads * wide(rows, p.many), own);
+  if (p.many) {
+    // whole rounds of workgroups that each take all keys of a tile; the rest is cut up
+    const int64_t rest = items % kShSlots;
+    p.tail = rest <= 400 ? rest : 0;
+    p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * rest + kShSlots - 1) / kShSlots);
+  } else {
+    p.tail = items;
+    p.chunk = std::max<int64_t>(getenv("CMIN") ? atoi(getenv("CMIN")) : 2, (steps * items + (getenv("CN") ? atoi(getenv("CN")) : 2048) - 1) / (getenv("CN") ? atoi(getenv("CN")) : 2048));
+  }
+  p.nsplit = std::max<int64_t>(1, (steps + p.chunk - 1) / p.chunk);
+  if (p.nsplit == 1 && p.gsplit == 0 && !p.stored) p.tail = 0;   // nothing to join
+  if (p.tail == 0) p.nsplit = 1;
+  p.full = items - p.tail;
   return p;
 }
-static int64_t part_bytes(const SharedShape& s, const SharedPlan& p) {
-  if (!p.join()) return 0;
-  const int64_t n = s.groups * s.kv_heads * p.gtiles * p.gsplit + s.batch * s.kv_heads * p.tiles * p.nsplit;
-  return n * (96 + 32 * s.dim) * 4;
+
+static int64_t slot_tiles(const SharedShape& s) { return (s.skv + kWeighSlots - 1) / kWeighSlots; }
+static int64_t weigh_chunks(const SharedShape& s) { return (s.sq * s.group() + kWeighRows - 1) / kWeighRows; }
+static bool weigh_shape_ok(const SharedShape& s) {
+  return s.batch * s.kv_heads * slot_tiles(s) < (1 << 24) &&
+         s.batch * s.kv_heads * slot_tiles(s) * weigh_chunks(s) < (1 << 24);
 }
-static int64_t shared_ws_bytes(const SharedShape& s, bool weigh) {
-  return part_bytes(s, shared_plan(s)) + (weigh ? stats_bytes(s) : 0);
+
+// The workspace: parts, then what the weights need.
+struct SharedSpace {
+  int64_t part, stats, scores, sums;
+  int64_t total() const { return part + stats + scores + sums; }
+};
+static SharedSpace shared_space(const SharedShape& s, const SharedPlan& p, bool weigh) {
+  SharedSpace x{};
+  const int64_t heads = s.batch * s.kv_heads;
+  const int64_t n = s.groups * s.kv_heads * p.gtiles * p.gsplit + p.tail * (p.many ? kShWaves : 1) * p.nsplit;
+  if (p.gsplit > 0 || p.tail > 0) x.part = n * (96 + 32 * s.dim) * 4;
+  if (!weigh) return x;
+  if (p.stored) {
+    x.scores = heads * s.sq * s.group() * score_row(s.skv) * 4;
+  } else {
+    x.stats = heads * 32 * p.tiles * 8 + 1024;       // whole blocks of 128 rows are read
+    if (weigh_chunks(s) > 1) x.sums = (heads * weigh_chunks(s) * s.skv * 4 + 15) / 16 * 16;
+  }
+  return x;
 }
 
 template <int DT, int MODE, int D, bool WEIGH>
 static void launch_shared(const SharedShape& s, hipStream_t stream, const SharedArgs& g) {
   const int64_t heads = s.batch * s.kv_heads;
   const dim3 block(64 * kShWaves);
-  const int64_t own = heads * (g.many ? (g.tiles + kShWaves - 1) / kShWaves : g.tiles) * g.nsplit;
-  hipLaunchKernelGGL((shared_kernel<DT, MODE, D, WEIGH>), dim3((uint32_t)(g.gwork + own)), block, 0, stream, g);
-  if (g.gsplit > 0 || g.nsplit > 1) {
-    if (g.gsplit + g.nsplit > kShJoinFew)
-      hipLaunchKernelGGL((shared_join_kernel<DT, D, WEIGH, true>), dim3((uint32_t)(heads * g.tiles * 32)),
-                         dim3(256), 0, stream, g);
-    else
-      hipLaunchKernelGGL((shared_join_kernel<DT, D, WEIGH, false>), dim3((uint32_t)(heads * g.tiles * D / 32)),
-                         dim3(256), 0, stream, g);
+  const uint32_t work = g.gwork + g.full + g.tail * (uint32_t)g.nsplit;
+  hipLaunchKernelGGL((shared_kernel<DT, MODE, D, WEIGH>), dim3(work), block, 0, stream, g);
+  const bool stored = WEIGH && g.scores != nullptr;
+  if (g.tail > 0) {
+    const uint32_t slots = stored ? (uint32_t)((s.skv + kScoreSlots - 1) / kScoreSlots) : 0u;
+    const int64_t rows = (int64_t)g.tail * (g.many ? 32 * kShWaves : 32);
+    const auto launch = [&](auto teams) {
+      constexpr int T = decltype(teams)::value, R = 1024 / D / T;
+      const uint32_t joins = (uint32_t)((rows + R - 1) / R);
+      hipLaunchKernelGGL((shared_join_kernel<DT, MODE, D, WEIGH, T>), dim3(joins + (uint32_t)heads * slots), dim3(256), 0,
+                         stream, g, joins, slots);
+    };
+    const int32_t parts = g.gsplit + g.nsplit;
+    if (parts <= 16) launch(std::integral_constant<int, 1>{});
+    else launch(std::integral_constant<int, 8>{});
   }
-  const uint32_t n = (uint32_t)slot_tiles(s);
-  if constexpr (WEIGH)
-    if (n > 0)
-      hipLaunchKernelGGL((weigh_rows_kernel<DT, MODE, D>), dim3((uint32_t)heads * n), block, 0, stream, g, n);
+  if constexpr (WEIGH) {
+    const uint32_t n = (uint32_t)slot_tiles(s), chunks = (uint32_t)weigh_chunks(s);
+    if (stored || n == 0) return;
+    hipLaunchKernelGGL((weigh_rows_kernel<DT, MODE, D>), dim3((uint32_t)heads * n * chunks), block, 0, stream, g, n, chunks);
+    if (chunks > 1) {
+      const uint32_t blocks = (uint32_t)((s.skv + 255) / 256);
+      hipLaunchKernelGGL(weigh_add_kernel, dim3((uint32_t)heads * blocks), dim3(256), 0, stream, g, blocks, chunks);
+    }
+  }
 }
 template <int DT, int D, bool WEIGH>
 static void launch_shared(int mode, const SharedShape& s, hipStream_t stream, const SharedArgs& g) {
@@ -815,7 +1078,7 @@ extern "C" quake_status quake_attention_shared_workspace_size(int64_t batch, int
                                                               int64_t* bytes) {
   const SharedShape s{batch, groups, sq, sp, skv, heads, kv_heads, dim};
   if (bytes == nullptr || !shared_shape_ok(s) || (weigh && !weigh_shape_ok(s))) return QUAKE_EINVAL;
-  *bytes = shared_ws_bytes(s, weigh != 0);
+  *bytes = shared_space(s, shared_plan(s, weigh != 0, true), weigh != 0).total();
   return QUAKE_OK;
 }
 
@@ -863,7 +1126,9 @@ extern "C" quake_status quake_attention_shared(
     if (!rows_apart(sw, nw, 2, skv)) return QUAKE_EINVAL;
     if (workspace == nullptr) return QUAKE_EINVAL;
   }
-  const int64_t need = shared_ws_bytes(s, weigh);
+  const SharedPlan p = shared_plan(s, weigh, workspace != nullptr);
+  const SharedSpace space = shared_space(s, p, weigh);
+  const int64_t need = space.total();
   if (workspace != nullptr && need > 0) {
     if (workspace_bytes < need) return QUAKE_EINVAL;
     if (meet(workspace, need, q, span_bytes(st.q, nq, 3, dim, 2)) ||
@@ -888,12 +1153,11 @@ extern "C" quake_status quake_attention_shared(
   g.prefix_lens = prefix_lens;
   g.q_lens = q_lens;
   g.kv_lens = kv_lens;
-  SharedPlan p;
-  p.tiles = s.tiles();
-  if (workspace != nullptr) p = shared_plan(s);
-  else p.many = s.sq * s.group() >= 96;
-  g.part = static_cast<float*>(workspace);
-  g.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + part_bytes(s, p));
+  char* ws = static_cast<char*>(workspace);
+  g.part = reinterpret_cast<float*>(ws);
+  if (space.stats > 0) g.stats = reinterpret_cast<float2*>(ws + space.part);
+  if (space.scores > 0) g.scores = reinterpret_cast<float*>(ws + space.part + space.stats);
+  if (space.sums > 0) g.sums = reinterpret_cast<float*>(ws + space.part + space.stats + space.scores);
   g.st = st;
   g.sq = (int32_t)sq;
   g.sp = (int32_t)sp;
@@ -901,14 +1165,22 @@ extern "C" quake_status quake_attention_shared(
   g.group = (int32_t)s.group();
   g.kv_heads = (int32_t)kv_heads;
   g.members = (int32_t)(batch / groups);
+  g.pkt = (int32_t)st.prefix_k[1];
+  g.pvt = (int32_t)st.prefix_v[1];
+  g.kt = (int32_t)st.k[1];
+  g.vt = (int32_t)st.v[1];
   g.groups = (int32_t)groups;
   g.gtiles = (int32_t)p.gtiles;
-  g.gsplit = (int32_t)p.gsplit;
   g.gmany = p.gmany;
+  g.gchunk = (int32_t)p.gchunk;
+  g.gsplit = (int32_t)p.gsplit;
+  g.gwork = (uint32_t)(p.gitems * p.gsplit);
   g.tiles = (int32_t)p.tiles;
-  g.nsplit = (int32_t)p.nsplit;
   g.many = p.many;
-  g.gwork = (uint32_t)(groups * kv_heads * (p.gmany ? (p.gtiles + kShWaves - 1) / kShWaves : p.gtiles) * p.gsplit);
+  g.chunk = (int32_t)p.chunk;
+  g.nsplit = (int32_t)p.nsplit;
+  g.full = (uint32_t)p.full;
+  g.tail = (uint32_t)p.tail;
   g.c0 = c0;
   const hipStream_t on = static_cast<hipStream_t>(stream);
   if (dtype == QUAKE_BF16) {
