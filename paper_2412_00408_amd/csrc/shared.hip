@@ -686,12 +686,22 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
   constexpr int C = D / 4, TEAMS = 256 / C, R = TEAMS / T, U = 4;
   const int team = threadIdx.x / C, c = threadIdx.x % C, k = team % T;   // team k of its row
   const uint32_t n = block * R + team / T;                               // row of all that are joined
-  const uint32_t per = g.many ? 32 * kShWaves : 32;
-  const uint32_t id = g.full + n / per;
-  const TileOf t = tile_of(g, id);
-  const int b = (int)(t.bh / (uint32_t)g.kv_heads), hk = (int)(t.bh % (uint32_t)g.kv_heads);
-  const int32_t row = t.tile * (int32_t)per + (int32_t)(n % per);
-  const bool in = n / per < g.tail;
+  // tiles of 128 rows from the first one that is cut; else all rows of all key heads
+  const uint32_t per = g.many ? 32 * kShWaves : (uint32_t)(g.sq * g.group);
+  const uint32_t item = n / per;
+  int32_t row = (int32_t)(n - item * per);
+  uint32_t id = g.full + item, bh = item;
+  bool in;
+  if (g.many) {
+    const TileOf t = tile_of(g, id);
+    bh = t.bh;
+    row += t.tile * (int32_t)per;
+    in = item < g.tail;
+  } else {
+    id = bh * (uint32_t)g.tiles + (uint32_t)(g.tiles - 1 - (row >> 5));
+    in = item * (uint32_t)g.tiles < g.tail;
+  }
+  const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)(bh - (uint32_t)b * g.kv_heads);
   const int32_t qlen = in ? seq_len(g.q_lens, b, g.sq) : 0, rows = qlen * g.group;
   const bool live = row < rows;
   float m = kNoMax, sum = 0.0f, every = 0.0f;
@@ -708,7 +718,7 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
     m = top;
   };
   if (live) {
-    const Parts p = parts_of<D>(g, id, t.bh, b, row, rows, seq_len(g.kv_lens, b, g.skv) - qlen);
+    const Parts p = parts_of<D>(g, id, bh, b, row, rows, seq_len(g.kv_lens, b, g.skv) - qlen);
     for (int32_t s0 = k; s0 < p.n; s0 += U * T) {
       float om[U], os[U], oe[U];
       float4 ov[U];
@@ -742,7 +752,7 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
   if (!live) return;
   if constexpr (WEIGH) {
     if (c == 0 && g.scores == nullptr)
-      g.stats[(int64_t)t.bh * 32 * g.tiles + row] = every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
+      g.stats[(int64_t)bh * 32 * g.tiles + row] = every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   uint16_t* orow = g.o + b * g.st.o[0] + (row / g.group) * g.st.o[1] + (hk * g.group + row % g.group) * g.st.o[2];
@@ -1030,7 +1040,7 @@ static void launch_shared(const SharedShape& s, hipStream_t stream, const Shared
   const bool stored = WEIGH && g.scores != nullptr;
   if (g.tail > 0) {
     const uint32_t slots = stored ? (uint32_t)((s.skv + kScoreSlots - 1) / kScoreSlots) : 0u;
-    const int64_t rows = (int64_t)g.tail * (g.many ? 32 * kShWaves : 32);
+    const int64_t rows = g.many ? (int64_t)g.tail * 32 * kShWaves : heads * s.sq * s.group();
     const auto launch = [&](auto teams) {
       constexpr int T = decltype(teams)::value, R = 1024 / D / T;
       const uint32_t joins = (uint32_t)((rows + R - 1) / R);
