@@ -31,187 +31,280 @@ struct EvictArgs {
   int32_t *kept, *evicted;
   quake_evict_strides st;                  // k's and v's in bytes here
   int32_t skv, slots, kv_heads, budget, sinks, recent;
-  int32_t row16, slice, slices;            // 16-byte chunks of a row, of a slice; slices of a row
+  int32_t row16, slice, slices;            // 16-byte chunks of a row; in place: chunks of a slice of
+                                           // it, slices of a row, else rows of a run, runs
 };
 
-constexpr int kEvThreads = 1024, kEvWaves = kEvThreads / 64, kEvBins = 2048;
-
-// weights in ascending order as unsigned: NaN below all, -0 as 0
+// Weights in ascending order as unsigned numbers: NaN below all, -0 as 0. What is kept
+// whatever its weight is above all, what is no slot below all.
+constexpr uint32_t kAlways = 0xFFFFFFFFu, kNever = 0u;
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  if (w != w) return 0u;
+  if (w != w) return 1u;
   const uint32_t u = as_u(w == 0.0f ? 0.0f : w);
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// One workgroup a sequence and key head.
-__global__ __launch_bounds__(kEvThreads) void evict_choose_kernel(EvictArgs g) {
-  __shared__ uint32_t s_bin[kEvBins];
-  __shared__ uint32_t s_wave[kEvWaves], s_eq[kEvWaves], s_found[2];
+// A workgroup a sequence and key head; a wave has a run of the slots. The key of the last one
+// that fits comes digit by digit from the top (11, 11 and 10 bits), by counting in LDS those
+// whose upper digits are the key's. Up to kHeld slots a thread stay in registers, longer rows
+// are read again for each digit and twice for the result. One compute unit's instructions
+// and barriers bound it.
+constexpr int kBins = 2048, kHeld = 16, kEach = 8;
+
+template <int THREADS>
+struct ChooseShared {
+  uint32_t bins[3][kBins];
+  uint32_t wave[THREADS / 64], equal[THREADS / 64], found[2];
+};
+
+template <int THREADS, bool HELD>
+__device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w, int32_t len, int32_t* kept,
+                                             ChooseShared<THREADS>& sh) {
+  constexpr int E = HELD ? kHeld : kEach, W = THREADS / 64, N = kBins / THREADS;   // bins a thread
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int hk = blockIdx.x % (uint32_t)g.kv_heads, b = blockIdx.x / (uint32_t)g.kv_heads;
+  const int32_t lo = g.sinks, hi = len - g.recent;
+  const int32_t run = (len + THREADS - 1) / THREADS * 64;
+  const int32_t from = wave * run, to = min(from + run, len);
+  uint32_t u[E];
+  const auto fetch = [&](int32_t i0) {
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int32_t i = i0 + 64 * e + lane;
+      x[e] = i < to ? w[i] : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int32_t i = i0 + 64 * e + lane;
+      u[e] = i >= to ? kNever : i < lo || i >= hi ? kAlways : weight_key(x[e]);
+    }
+  };
+  const auto each = [&](auto f) {      // f(slot of lane 0, this lane's key), of this wave's run
+    for (int32_t i0 = from; i0 < to; i0 += 64 * E) {
+      if (!HELD) fetch(i0);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (i0 + 64 * e < to) f(i0 + 64 * e, u[e]);
+    }
+  };
+  if (HELD) fetch(from);
+  for (int i = threadIdx.x; i < 3 * kBins; i += THREADS) sh.bins[0][i] = 0;
+  __syncthreads();
+  uint32_t key = 0, left = (uint32_t)g.budget;       // of the slots whose upper digits are key's
+  const auto digit = [&](uint32_t* bins, int shift, uint32_t mask, uint32_t upper) {
+    each([&](int32_t, uint32_t k) {
+      if ((k & upper) == key) atomicAdd(&bins[(k >> shift) & mask], 1u);
+    });
+    __syncthreads();
+    // thread t: N bins from the top
+    const int top = kBins - 1 - N * (int)threadIdx.x;
+    uint32_t c[N], mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine += c[i] = bins[top - i];
+    uint32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t other = __shfl_up(upto, o, 64);
+      upto += lane >= o ? other : 0u;
+    }
+    if (lane == 63) sh.wave[wave] = upto;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) upto += i < wave ? sh.wave[i] : 0u;
+    uint32_t above = upto - mine;                    // in the bins above this thread's
+    if (above < left && left <= upto) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (above < left && left <= above + c[i]) {
+          sh.found[0] = (uint32_t)(top - i);
+          sh.found[1] = above;
+        }
+        above += c[i];
+      }
+    }
+    __syncthreads();
+    key |= sh.found[0] << shift;
+    left -= sh.found[1];
+  };
+  digit(sh.bins[0], 21, 0x7FFu, 0u);
+  digit(sh.bins[1], 10, 0x7FFu, 0xFFE00000u);
+  digit(sh.bins[2], 0, 0x3FFu, 0xFFFFFC00u);
+  // kept slots in order: those above the key and, of its equals, the first `left`
+  uint32_t n = 0, ne = 0;
+  each([&](int32_t, uint32_t k) {
+    n += (uint32_t)__popcll(__ballot(k > key));
+    ne += (uint32_t)__popcll(__ballot(k == key));
+  });
+  if (lane == 0) {
+    sh.wave[wave] = n;
+    sh.equal[wave] = ne;
+  }
+  __syncthreads();
+  n = ne = 0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    n += i < wave ? sh.wave[i] : 0u;
+    ne += i < wave ? sh.equal[i] : 0u;
+  }
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  each([&](int32_t i, uint32_t k) {
+    const uint64_t more = __ballot(k > key), equal = __ballot(k == key);
+    const uint32_t rank = ne + (uint32_t)__popcll(equal & below);   // among the equal ones
+    if (k > key || (k == key && rank < left))
+      kept[n + (uint32_t)__popcll(more & below) + min(rank, left)] = i + lane;
+    n += (uint32_t)__popcll(more);
+    ne += (uint32_t)__popcll(equal);
+  });
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_choose_kernel(EvictArgs g) {
+  __shared__ ChooseShared<THREADS> sh;
+  const int b = (int)(blockIdx.x / (uint32_t)g.kv_heads), hk = (int)blockIdx.x - b * g.kv_heads;
   const int32_t len = seq_len(g.lens, b, g.skv);
   int32_t* kept = g.kept + (int64_t)blockIdx.x * g.budget;
   if (hk == 0 && threadIdx.x == 0) g.evicted[b] = max(len - g.budget, 0);
   if (len <= g.budget) {
-    for (int32_t i = threadIdx.x; i < g.budget; i += kEvThreads) kept[i] = i < len ? i : -1;
+    for (int32_t i = threadIdx.x; i < g.budget; i += THREADS) kept[i] = i < len ? i : -1;
     return;
   }
   const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
-  const int32_t lo = g.sinks, hi = len - g.recent;
-  // the key of the last one that fits, and how many of its equals do
-  uint32_t key = 0xFFFFFFFFu, left = (uint32_t)(g.budget - g.sinks - g.recent);
-  if (left > 0) {
-    uint32_t mask = 0;
-    key = 0;
-    for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
-      const uint32_t digit = shift == 0 ? 0x3FFu : 0x7FFu;
-      for (int i = threadIdx.x; i < kEvBins; i += kEvThreads) s_bin[i] = 0;
-      __syncthreads();
-      for (int32_t i = lo + (int32_t)threadIdx.x; i < hi; i += kEvThreads) {
-        const uint32_t u = weight_key(w[i]);
-        if ((u & mask) == key) atomicAdd(&s_bin[(u >> shift) & digit], 1u);
-      }
-      __syncthreads();
-      // thread t: bins 2047 - 2 t and the one below, from the top
-      const int top = kEvBins - 1 - 2 * (int)threadIdx.x;
-      const uint32_t a = s_bin[top], z = s_bin[top - 1];
-      uint32_t upto = a + z;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t other = __shfl_up(upto, o, 64);
-        upto += lane >= o ? other : 0u;
-      }
-      if (lane == 63) s_wave[wave] = upto;
-      __syncthreads();
-      for (int i = 0; i < wave; ++i) upto += s_wave[i];
-      const uint32_t above = upto - a - z;          // in the bins above both
-      if (above < left && left <= upto) {
-        const bool first = left <= above + a;
-        s_found[0] = (uint32_t)(first ? top : top - 1);
-        s_found[1] = first ? above : above + a;
-      }
-      __syncthreads();
-      key |= s_found[0] << shift;
-      mask |= digit << shift;
-      left -= s_found[1];
-    }
-  }
-  // kept slots in order; a wave takes a run of them
-  const int32_t run = (len + kEvThreads - 1) / kEvThreads * 64;
-  const int32_t from = wave * run, to = min(from + run, len);
-  auto look = [&](int32_t i, uint64_t& more, uint64_t& equal) {
-    const bool in = i < to, mid = in && i >= lo && i < hi;
-    const uint32_t u = mid ? weight_key(w[i]) : 0u;
-    more = __ballot(in && (!mid || u > key));
-    equal = __ballot(mid && u == key && left > 0);
-  };
-  uint32_t n = 0, ne = 0;
-  for (int32_t i = from; i < to; i += 64) {
-    uint64_t more, equal;
-    look(i + lane, more, equal);
-    n += (uint32_t)__popcll(more);
-    ne += (uint32_t)__popcll(equal);
-  }
-  __syncthreads();
-  if (lane == 0) {
-    s_wave[wave] = n;
-    s_eq[wave] = ne;
-  }
-  __syncthreads();
-  n = ne = 0;
-  for (int i = 0; i < wave; ++i) {
-    n += s_wave[i];
-    ne += s_eq[i];
-  }
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int32_t i = from; i < to; i += 64) {
-    uint64_t more, equal;
-    look(i + lane, more, equal);
-    const uint32_t rank = ne + (uint32_t)__popcll(equal & below);   // among the equal ones
-    const bool mine = ((more >> lane) & 1) != 0 || (((equal >> lane) & 1) != 0 && rank < left);
-    const uint32_t at = n + (uint32_t)__popcll(more & below) + min(rank, left);
-    if (mine) kept[at] = i + lane;
-    n += (uint32_t)__popcll(more);
-    ne += (uint32_t)__popcll(equal);
-  }
+  if (len <= kHeld * THREADS)
+    choose_slots<THREADS, true>(g, w, len, kept, sh);
+  else
+    choose_slots<THREADS, false>(g, w, len, kept, sh);
 }
 
-constexpr int kMvThreads = 256, kMvEach = 4;
+// The weights of a key head, and the sequence's length.
+constexpr int kMvEach = 4;
 
-// A slice of the rows of K or V of one key head, or its weights, by one workgroup.
-__global__ __launch_bounds__(kMvThreads) void evict_move_kernel(EvictArgs g) {
-  const uint32_t parts = 2u * (uint32_t)g.slices + 1u;
-  const uint32_t part = blockIdx.x % parts, bh = blockIdx.x / parts;
-  const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
-  const int32_t* kept = g.kept + (int64_t)bh * g.budget;
-  if (part == parts - 1u) {
-    const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
-    float* wo = g.wo + b * g.st.weight_out[0] + hk * g.st.weight_out[1];
-    int32_t n = 0;                                   // kept
-    for (int32_t i0 = 0; i0 < g.budget; i0 += kMvThreads * kMvEach) {
-      float x[kMvEach];
-      int32_t live = 0;
-#pragma unroll
-      for (int j = 0; j < kMvEach; ++j) {
-        const int32_t i = i0 + j * kMvThreads + (int32_t)threadIdx.x;
-        const int32_t from = i < g.budget ? kept[i] : -1;
-        x[j] = from >= 0 ? w[from] : 0.0f;
-        live += from >= 0;
-      }
-      n += live;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kMvEach; ++j) {
-        const int32_t i = i0 + j * kMvThreads + (int32_t)threadIdx.x;
-        if (i < g.budget) wo[i] = x[j];
-      }
-    }
-    for (int32_t i = g.budget + (int32_t)threadIdx.x; i < g.slots; i += kMvThreads) wo[i] = 0.0f;
-    if (hk == 0 && g.lens_out != nullptr) {
-      __shared__ int32_t s_n[kMvThreads / 64];
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
-      if ((threadIdx.x & 63) == 0) s_n[threadIdx.x >> 6] = n;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        for (int i = 1; i < kMvThreads / 64; ++i) n += s_n[i];
-        g.lens_out[b] = n;
-      }
-    }
-    return;
-  }
-  const bool value = part >= (uint32_t)g.slices;
-  const uint32_t c0 = (part - (value ? (uint32_t)g.slices : 0u)) * (uint32_t)g.slice;
-  const int64_t* si = value ? g.st.v : g.st.k;
-  const int64_t* so = value ? g.st.v_out : g.st.k_out;
-  const char* src = (value ? g.v : g.k) + b * si[0] + hk * si[2];
-  char* dst = (value ? g.vo : g.ko) + b * so[0] + hk * so[2];
-  const bool same = src == dst;
-  const int64_t ss = si[1], sd = so[1];
-  const uint32_t width = min((uint32_t)g.slice, (uint32_t)g.row16 - c0);
-  const uint64_t all = (uint64_t)g.budget * width;
-  for (uint64_t e0 = 0; e0 < all; e0 += kMvThreads * kMvEach) {
-    u32x4 x[kMvEach];
+template <int THREADS>
+__device__ __forceinline__ void move_weights(const EvictArgs& g, int b, int hk, const int32_t* kept) {
+  const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
+  float* wo = g.wo + b * g.st.weight_out[0] + hk * g.st.weight_out[1];
+  int32_t n = 0;                                     // kept
+  for (int32_t i0 = 0; i0 < g.budget; i0 += THREADS * kMvEach) {
+    float x[kMvEach];
     int32_t from[kMvEach];
 #pragma unroll
     for (int j = 0; j < kMvEach; ++j) {
-      const uint64_t e = e0 + (uint32_t)(j * kMvThreads) + threadIdx.x;
-      const int32_t i = (int32_t)(e / width);
-      const uint32_t c = (uint32_t)(e % width);
-      from[j] = e < all ? kept[i] : -1;
-      if (same && from[j] == i) from[j] = -1;        // stays where it is
-      if (from[j] >= 0) x[j] = *reinterpret_cast<const u32x4*>(src + from[j] * ss + 16 * (int64_t)(c0 + c));
+      const int32_t i = i0 + j * THREADS + (int32_t)threadIdx.x;
+      from[j] = i < g.budget ? kept[i] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kMvEach; ++j) {
+      x[j] = from[j] >= 0 ? w[from[j]] : 0.0f;
+      n += from[j] >= 0;
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kMvEach; ++j) {
-      const uint64_t e = e0 + (uint32_t)(j * kMvThreads) + threadIdx.x;
-      const int32_t i = (int32_t)(e / width);
-      const uint32_t c = (uint32_t)(e % width);
-      if (from[j] >= 0) *reinterpret_cast<u32x4*>(dst + i * sd + 16 * (int64_t)(c0 + c)) = x[j];
+      const int32_t i = i0 + j * THREADS + (int32_t)threadIdx.x;
+      if (i < g.budget) wo[i] = x[j];
     }
   }
+  for (int32_t i = g.budget + (int32_t)threadIdx.x; i < g.slots; i += THREADS) wo[i] = 0.0f;
+  if (hk > 0 || g.lens_out == nullptr) return;
+  __shared__ int32_t s_n[THREADS / 64];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) s_n[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < THREADS / 64; ++i) n += s_n[i];
+    g.lens_out[b] = n;
+  }
+}
+
+// Rows [i, end) of a slice of K or V of one key head; IN: in place, a round's rows are all read
+// before one is written, and the next round's are on their way meanwhile.
+template <int THREADS, int EACH, bool IN>
+__device__ __forceinline__ void move_rows(const EvictArgs& g, const char* src, char* dst, int64_t ss, int64_t sd,
+                                          const int32_t* kept, int32_t i, int32_t end, uint32_t c0, uint32_t width) {
+  const uint32_t rows = THREADS / width;             // at a time; the last threads may have none
+  const uint32_t r = threadIdx.x / width, c = threadIdx.x - r * width;
+  const bool has = r < rows;
+  src += 16 * (int64_t)(c0 + c);
+  dst += 16 * (int64_t)(c0 + c);
+  struct Round {
+    int32_t from[EACH];
+    u32x4 x[EACH];
+  };
+  const auto read = [&](Round& q, int32_t at) {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int32_t k = at + (int32_t)(j * rows + r);
+      q.from[j] = has && k < end ? kept[k] : -1;
+      if (IN && q.from[j] == k) q.from[j] = -1;      // stays where it is
+    }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+      if (q.from[j] >= 0) q.x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + q.from[j] * ss));
+  };
+  const auto write = [&](const Round& q, int32_t at) {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int32_t k = at + (int32_t)(j * rows + r);
+      if (q.from[j] >= 0) __builtin_nontemporal_store(q.x[j], reinterpret_cast<u32x4*>(dst + k * sd));
+    }
+  };
+  const int32_t step = (int32_t)(EACH * rows);
+  Round a;
+  read(a, i);
+  for (; i < end; i += step) {
+    Round next;
+    read(next, i + step);
+    if (IN) {
+      // this round's reads are in registers, in every wave
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) asm volatile("" : "+v"(a.x[j]));
+      __syncthreads();
+    }
+    write(a, i);
+    a = next;
+  }
+}
+
+// In place: slices of rows, and the weights, a workgroup each.
+constexpr int kInThreads = 1024;
+__global__ __launch_bounds__(kInThreads) void evict_shift_kernel(EvictArgs g) {
+  const uint32_t parts = 2u * (uint32_t)g.slices + 1u;
+  const uint32_t bh = blockIdx.x / parts, part = blockIdx.x - bh * parts;
+  const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)bh - b * g.kv_heads;
+  const int32_t* kept = g.kept + (int64_t)bh * g.budget;
+  if (part == parts - 1u) {
+    move_weights<kInThreads>(g, b, hk, kept);
+    return;
+  }
+  const bool value = part >= (uint32_t)g.slices;
+  const uint32_t c0 = (part - (value ? (uint32_t)g.slices : 0u)) * (uint32_t)g.slice;
+  const int64_t* st = value ? g.st.v : g.st.k;
+  char* at = (value ? g.vo : g.ko) + b * st[0] + hk * st[2];
+  move_rows<kInThreads, kMvEach, true>(g, at, at, st[1], st[1], kept, 0, g.budget, c0,
+                                       min((uint32_t)g.slice, (uint32_t)g.row16 - c0));
+}
+
+// Into another cache: runs of g.run rows of K, of V, and the weights.
+constexpr int kCopyThreads = 256;
+__global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictArgs g) {
+  const uint32_t parts = 2u * (uint32_t)g.slices + 1u;
+  const uint32_t bh = blockIdx.x / parts, part = blockIdx.x - bh * parts;
+  const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)bh - b * g.kv_heads;
+  const int32_t* kept = g.kept + (int64_t)bh * g.budget;
+  if (part == parts - 1u) {
+    move_weights<kCopyThreads>(g, b, hk, kept);
+    return;
+  }
+  const bool value = part >= (uint32_t)g.slices;
+  const int32_t i = (int32_t)(part - (value ? (uint32_t)g.slices : 0u)) * g.slice;
+  const int64_t* si = value ? g.st.v : g.st.k;
+  const int64_t* so = value ? g.st.v_out : g.st.k_out;
+  const char* src = (value ? g.v : g.k) + b * si[0] + hk * si[2];
+  char* dst = (value ? g.vo : g.ko) + b * so[0] + hk * so[2];
+  for (uint32_t c0 = 0; c0 < (uint32_t)g.row16; c0 += kCopyThreads)
+    move_rows<kCopyThreads, kMvEach, false>(g, src, dst, si[1], so[1], kept, i, min(i + g.slice, g.budget), c0,
+                                            min((uint32_t)g.row16 - c0, (uint32_t)kCopyThreads));
 }
 
 }  // namespace qk
@@ -317,11 +410,27 @@ extern "C" quake_status quake_cache_evict(const void* k, const void* v, const fl
   g.sinks = (int32_t)sinks;
   g.recent = (int32_t)recent;
   g.row16 = (int32_t)(dim * e / 16);
-  const uint32_t heads = (uint32_t)(batch * kv_heads);
-  g.slice = heads >= 256 ? g.row16 : std::min(g.row16, 4);
-  g.slices = (g.row16 + g.slice - 1) / g.slice;
+  const int64_t heads = batch * kv_heads;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(evict_choose_kernel, dim3(heads), dim3(kEvThreads), 0, s, g);
-  hipLaunchKernelGGL(evict_move_kernel, dim3(heads * (2u * (uint32_t)g.slices + 1u)), dim3(kMvThreads), 0, s, g);
+  // four waves a row where its slots fit their registers, which leaves room for more rows
+  if (skv <= kHeld * 256)
+    hipLaunchKernelGGL(evict_choose_kernel<256>, dim3((uint32_t)heads), dim3(256), 0, s, g);
+  else
+    hipLaunchKernelGGL(evict_choose_kernel<1024>, dim3((uint32_t)heads), dim3(1024), 0, s, g);
+  if (k_out == k) {
+    // a row whole where there are heads enough, else in up to as many slices as fill the GPU
+    g.slice = (int32_t)std::max<int64_t>(g.row16 * 2 * heads / 512, std::min(g.row16, 4));
+    g.slice = std::min(g.slice, g.row16);
+    g.slices = (g.row16 + g.slice - 1) / g.slice;
+    hipLaunchKernelGGL(evict_shift_kernel, dim3((uint32_t)(heads * (2 * g.slices + 1))), dim3(kInThreads), 0, s, g);
+  } else {
+    // runs of about 64 KiB, of fewer where that leaves the GPU idle
+    int64_t rows = std::max<int64_t>(1, (1 << 16) / (dim * e));
+    rows = std::max<int64_t>(std::min(rows, budget * heads * 2 / 1024), std::max<int64_t>(1, 4096 / (dim * e)));
+    rows = std::max(rows, budget * heads / (1 << 22) + 1);       // a launch takes fewer than 2^32 threads
+    g.slice = (int32_t)std::min(rows, budget);
+    g.slices = (int32_t)((budget + g.slice - 1) / g.slice);
+    hipLaunchKernelGGL(evict_copy_kernel, dim3((uint32_t)(heads * (2 * g.slices + 1))), dim3(kCopyThreads), 0, s, g);
+  }
   return launch_status();
 }

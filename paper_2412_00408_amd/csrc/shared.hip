@@ -25,6 +25,21 @@ namespace qk {
 
 constexpr int kShWaves = 4;
 
+// Division by a number the host knows: n / d = floor(n m / 2^(32 + s)) for n < 2^31 with
+// 2^s < d <= 2^(s + 1), m = ceil(2^(32 + s) / d) < 2^32: n m / 2^(32 + s) exceeds n / d by less
+// than n / 2^(32 + s) <= 2^-(s + 1) <= 1 / d.
+struct Div {
+  uint32_t d = 1, m = 0, s = 0;
+  Div() = default;
+  explicit Div(int64_t by) : d((uint32_t)std::max<int64_t>(by, 1)) {
+    if (d == 1) return;
+    while (((uint64_t)2 << s) < d) ++s;
+    m = (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d);
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> s; }
+  __device__ __forceinline__ int32_t of(int32_t n) const { return (int32_t)of((uint32_t)n); }   // n >= 0
+};
+
 // A token's stride is below 2^24 + 1, so the strides that loops use are 32-bit ones.
 struct SharedArgs {
   const uint16_t *q, *pk, *pv, *k, *v;
@@ -38,12 +53,14 @@ struct SharedArgs {
   quake_shared_strides st;
   int32_t pkt, pvt, kt, vt;                     // token strides
   int32_t groups, sq, sp, skv, group, kv_heads, members;
-  int32_t gtiles, gmany, gchunk, gsplit;        // of a group's rows (gsplit 0: none) ..
-  int32_t tiles, many, chunk, nsplit;           // .. and a sequence's: tiles of 32 rows, whether 128
-                                                // rows share a workgroup, steps of 64 keys a
-                                                // workgroup takes, the most parts of a tile
-  uint32_t gwork, full, tail;                   // workgroups of groups' rows; a sequence's tiles that
+  int32_t gtiles, gmany, gsplit;                // of a group's rows (gsplit 0: none) ..
+  int32_t tiles, many, nsplit;                  // .. and a sequence's: tiles of 32 rows, whether 128
+                                                // rows share a workgroup, the most parts of a tile
+  uint32_t heads, gwork, full, tail;            // key heads of all sequences; workgroups of groups' rows; tiles that
                                                 // one workgroup takes, and those cut into parts
+  Div by_group, by_sq, by_members, by_heads;    // heads: key heads
+  Div by_gtiles, by_gsplit, by_tiles, by_tail;     // tiles: in units of one workgroup's
+  Div by_gper, by_per, by_rows;                 // blocks of a part; rows of a key head or, many, 128
   float c0;                                     // 2^23 t / ln2 (EXACT: t / ln2)
 };
 
@@ -67,13 +84,12 @@ __device__ __forceinline__ int32_t list_blocks(int32_t plen, int32_t own, bool m
   return many ? (plen + 63) / 64 + (own + 63) / 64 : (plen + 31) / 32 + (own + 31) / 32;
 }
 // parts that a list is cut into
-__device__ __forceinline__ int32_t list_parts(int32_t plen, int32_t own, bool many, int32_t chunk) {
-  const int32_t per = many ? chunk : 2 * chunk;
-  return (list_blocks(plen, own, many) + per - 1) / per;
+__device__ __forceinline__ int32_t list_parts(int32_t plen, int32_t own, bool many, const Div& per) {
+  return per.of(list_blocks(plen, own, many) + (int32_t)per.d - 1);
 }
 // own keys that the rows of the tile at r0 see
 __device__ __forceinline__ int32_t tile_keys(const SharedArgs& g, int32_t off, int32_t r0, int32_t rows) {
-  return max(off + min(r0 + (g.many ? 32 * kShWaves : 32) - 1, rows - 1) / g.group + 1, 0);
+  return rows == 0 ? 0 : max(off + g.by_group.of(min(r0 + (g.many ? 32 * kShWaves : 32), rows) - 1) + 1, 0);
 }
 __device__ __forceinline__ int32_t prefix_len(const SharedArgs& g, int32_t group) {
   return g.sp == 0 ? 0 : seq_len(g.prefix_lens, group, g.sp);
@@ -86,21 +102,41 @@ __device__ __forceinline__ int64_t group_part(const SharedArgs& g, int64_t bh, i
 __device__ __forceinline__ int64_t own_part(const SharedArgs& g, int64_t tile) {
   return (int64_t)g.groups * g.kv_heads * g.gtiles * g.gsplit + tile * g.nsplit;
 }
-// tile number `id` of the sequences (in units of one workgroup's): sequence, key head, tile;
-// those that see most first
-struct TileOf {
-  uint32_t bh;
-  int32_t tile;
-};
-__device__ __forceinline__ TileOf tile_of(const SharedArgs& g, uint32_t id) {
-  const uint32_t tiles = g.many ? ((uint32_t)g.tiles + kShWaves - 1) / kShWaves : (uint32_t)g.tiles;
-  return {id / tiles, (int32_t)(tiles - 1u - id % tiles)};
-}
 // Workgroups go round the 8 XCDs: number `at` of n as each XCD takes consecutive ones, which
 // share most of their keys, for its own L2.
 __device__ __forceinline__ uint32_t by_xcd(uint32_t at, uint32_t n) {
   const uint32_t x = at & 7u, per = n >> 3, rest = n & 7u;
   return x * per + min(x, rest) + (at >> 3);
+}
+// Number `at` of the sequences' tiles (in units of one workgroup's), in the order of their
+// launch: key head of a sequence, tile, those that see most first. The tiles of a key head
+// share an XCD, and key heads go round the XCDs one by one where they come out even: runs of
+// them would give one XCD the long sequences.
+struct TileOf {
+  uint32_t bh;
+  int32_t tile;
+};
+__device__ __forceinline__ TileOf tile_of(const SharedArgs& g, uint32_t at) {
+  const uint32_t tiles = g.by_tiles.d;
+  uint32_t id = at;
+  if (tiles > 1 && (g.heads & 7u) == 0) {
+    const uint32_t k = at >> 3, round = g.by_tiles.of(k);
+    return {8 * round + (at & 7u), (int32_t)(tiles - 1u - (k - round * tiles))};
+  }
+  if (tiles > 1) id = by_xcd(at, g.heads * tiles);
+  const uint32_t bh = g.by_tiles.of(id);
+  return {bh, (int32_t)(tiles - 1u - (id - bh * tiles))};
+}
+// The number of a key head's tile.
+__device__ __forceinline__ uint32_t number_of(const SharedArgs& g, uint32_t bh, int32_t tile) {
+  const uint32_t tiles = g.by_tiles.d, back = tiles - 1u - (uint32_t)tile;
+  if (tiles > 1 && (g.heads & 7u) == 0) return 8 * ((bh >> 3) * tiles + back) + (bh & 7u);
+  const uint32_t id = bh * tiles + back;
+  if (tiles == 1) return id;
+  // by_xcd's inverse
+  const uint32_t n = g.heads * tiles, per = n >> 3, rest = n & 7u, first = rest * (per + 1u);
+  const uint32_t x = id < first ? id / (per + 1u) : rest + (id - first) / per;
+  return 8 * (id - (x * per + min(x, rest))) + x;
 }
 struct RowOf {
   int32_t b, query, head, pos;
@@ -112,11 +148,11 @@ __device__ __forceinline__ RowOf row_of(const SharedArgs& g, const Work& w, int3
   x.live = r < w.rows;
   r = min(r, w.rows - 1);
   x.b = w.b;
-  x.query = r / g.group;
-  x.head = w.hk * g.group + r % g.group;
+  x.query = g.by_group.of(r);
+  x.head = w.hk * g.group + r - x.query * g.group;
   x.pos = w.off + x.query;
   if (w.whole) {
-    const int32_t m = x.query / g.sq;
+    const int32_t m = g.by_sq.of(x.query);
     x.b += m;
     x.query -= m * g.sq;
     x.pos = -1;
@@ -169,6 +205,22 @@ __device__ __forceinline__ void hide_behind(f32x16& s, int32_t n0, int32_t lim, 
   for (int r = 0; r < 16; ++r) s[r] = n0 + 8 * (r >> 2) + 4 * h + (r & 3) <= lim ? s[r] : -INFINITY;
 }
 
+// The exponential of `mode` times a constant that all of a row share, so that it cancels.
+// QuAKE2's is (a_m^2 + 2) / 3 with the exponent of z, which has the value 2^i a_m itself: 3/2
+// times it is one multiply-add, z (a_m / 2) + 2^i. An instruction less than with the mantissa
+// joined to the exponent, and two roundings.
+template <int MODE>
+__device__ __forceinline__ float row_exp(float x, float c0, float c1) {
+  if constexpr (MODE == Q2) {
+    uint32_t z;
+    const float l = __builtin_fmaf(x, c0, c1);
+    asm("v_cvt_u32_f32 %0, %1" : "=v"(z) : "v"(l));
+    return __builtin_fmaf(as_f(z), as_f((z & kMantMask) | 0x3F000000u), as_f(z & kSignExpMask));
+  } else {
+    return qexp_row<MODE, true>(x, c0, c1);
+  }
+}
+
 // sum of 16 values in pairs of pairs
 __device__ __forceinline__ float sum16(const float (&e)[16]) {
   float s[8];
@@ -185,7 +237,7 @@ __device__ __forceinline__ float sum16(const float (&e)[16]) {
 struct Lists {
   const uint16_t *pk, *pv, *k, *v;
   __device__ __forceinline__ Lists(const SharedArgs& g, const Work& w) {
-    const int32_t grp = w.b / g.members;
+    const int32_t grp = g.by_members.of(w.b);
     pk = g.pk + grp * g.st.prefix_k[0] + w.hk * g.st.prefix_k[2];
     pv = g.pv + grp * g.st.prefix_v[0] + w.hk * g.st.prefix_v[2];
     k = g.k + w.b * g.st.k[0] + w.hk * g.st.k[2];
@@ -213,10 +265,8 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const RowOf x = row_of(g, w, w.r0 + fr);
   if (!__any(x.live)) return;
-  u32x4 qf[D / 16];
-  load_q<D>(g, x, h, qf);
   const Lists lists(g, w);
-  const int32_t first = w.off + w.r0 / g.group;     // position of the first row
+  const int32_t first = w.off + g.by_group.of(w.r0);     // position of the first row
   const int32_t pblocks = (w.plen + 31) >> 5;
   const int32_t n_lo = w.n_lo, n_hi = w.n_hi;
   float* scores = nullptr;                          // of this lane's row, for the weights
@@ -243,6 +293,8 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     load_k(n_lo + wave);
     load_v(n_lo + wave);
   }
+  u32x4 qf[D / 16];
+  load_q<D>(g, x, h, qf);
   bool stored = false;
   for (int32_t n = n_lo + wave; n < n_hi; n += kShWaves) {
     const bool more = n + kShWaves < n_hi;
@@ -274,22 +326,16 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     }
     const float c1 = row_c1<MODE>(acc.m);
     u32x4 pr[2];
-    if constexpr (WEIGH) {
-      float e[16];
+    float e[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) e[r] = qexp_row<MODE, true>(s[r], g.c0, c1);
+    for (int r = 0; r < 16; ++r) e[r] = row_exp<MODE>(s[r], g.c0, c1);
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const uint32_t pair = wpack<DT>(e[r], e[r + 1]);
-        acc.sum = wsum<DT>(pair, acc.sum);
-        pr[r >> 3][(r >> 1) & 3] = pair;
-      }
-      all += sum16(e);
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; r += 2)
-        pr[r >> 3][(r >> 1) & 3] = prob_pair<DT, MODE>(s, r, g.c0, c1, acc.sum);
+    for (int r = 0; r < 16; r += 2) {                // summed as rounded: numerator and denominator
+      const uint32_t pair = wpack<DT>(e[r], e[r + 1]);   // share the rounding
+      acc.sum = wsum<DT>(pair, acc.sum);
+      pr[r >> 3][(r >> 1) & 3] = pair;
     }
+    if constexpr (WEIGH) all += sum16(e);
     // V is here; the next K and the scores may be on their way
     if (!more)
       wait_loads<0>();
@@ -306,73 +352,67 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     if (more) load_v(n + kShWaves);
   }
 
-  // join the waves: their M, then sums and O^T brought to the largest M
+  // join the waves: their M, then sums and O^T brought to the largest M; the rows of the
+  // tile alone, four dims a lane
   float (*s_m)[32] = reinterpret_cast<float (*)[32]>(s_row);
   float (*s_sum)[32] = s_m + kShWaves, (*s_all)[32] = s_sum + kShWaves;
   acc.sum += other_half(acc.sum);
   if constexpr (WEIGH) all += other_half(all);
-  __syncthreads();
-  if (lane < 32) {
-    s_m[wave][fr] = acc.m;
-    s_sum[wave][fr] = acc.sum;
-    if constexpr (WEIGH) s_all[wave][fr] = all;
-  }
-  float* mine = reinterpret_cast<float*>(s_buf + wave * kWave);   // [D][32] floats
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      mine[(32 * d + 8 * (r >> 2) + 4 * h + (r & 3)) * 32 + fr] = acc.o[d][r];
-  __syncthreads();
-  float m = s_m[0][fr];
-#pragma unroll
-  for (int i = 1; i < kShWaves; ++i) m = fmaxf(m, s_m[i][fr]);
-  float sum = 0.0f, every = 0.0f;
-  int32_t e[kShWaves];
-#pragma unroll
-  for (int i = 0; i < kShWaves; ++i) {
-    e[i] = down_shift(s_m[i][fr], m);
-    sum += __builtin_amdgcn_ldexpf(s_sum[i][fr], e[i]);
-    if constexpr (WEIGH) every += __builtin_amdgcn_ldexpf(s_all[i][fr], e[i]);
-  }
-  // this wave's dims: D / 4, each half of its lanes D / 8 of them
-  constexpr int N = D / 8;
-  const int d0 = wave * (D / 4) + h * N;
-  float v[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < kShWaves; ++j)
-      v[i] += __builtin_amdgcn_ldexpf(
-          reinterpret_cast<const float*>(s_buf + j * kWave)[(d0 + i) * 32 + fr], e[j]);
-  }
-  if (!x.live) return;
-  if (w.part >= 0) {
-    float* to = g.part + w.part * kPart<D>;
-    if (wave == 0 && h == 0) {
-      to[fr] = m;
-      to[32 + fr] = sum;
-      if constexpr (WEIGH) to[64 + fr] = every;
+  const int32_t rows = min(32, w.rows - w.r0);
+  constexpr int C = D / 4;                          // chunks of a row, swizzled
+  if (fr < rows) {
+    if (h == 0) {
+      s_m[wave][fr] = acc.m;
+      s_sum[wave][fr] = acc.sum;
+      if constexpr (WEIGH) s_all[wave][fr] = all;
     }
-    float4* wo = reinterpret_cast<float4*>(to + 96 + fr * D + d0);
+    float4* mine = reinterpret_cast<float4*>(buf) + fr * C;
 #pragma unroll
-    for (int i = 0; i < N; i += 4) wo[i / 4] = float4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-    return;
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        mine[(8 * d + 2 * i + h) ^ (fr & 7)] =
+            float4{acc.o[d][4 * i], acc.o[d][4 * i + 1], acc.o[d][4 * i + 2], acc.o[d][4 * i + 3]};
   }
-  if constexpr (WEIGH) {
-    if (wave == 0 && h == 0)
-      g.stats[((int64_t)w.b * g.kv_heads + w.hk) * 32 * g.tiles + w.r0 + fr] =
-          every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
-  }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  uint16_t* orow = g.o + x.b * g.st.o[0] + x.query * g.st.o[1] + x.head * g.st.o[2] + d0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * C; i += 64 * kShWaves) {
+    const int r = i / C, c = i % C;
+    float m = s_m[0][r];
 #pragma unroll
-  for (int i = 0; i < N; i += 8) {
-    u32x4 y;
+    for (int j = 1; j < kShWaves; ++j) m = fmaxf(m, s_m[j][r]);
+    float sum = 0.0f, every = 0.0f;
+    float4 v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = wpack<DT>(v[i + 2 * j] * inv, v[i + 2 * j + 1] * inv);
-    *reinterpret_cast<u32x4*>(orow + i) = y;
+    for (int j = 0; j < kShWaves; ++j) {
+      const int32_t e = down_shift(s_m[j][r], m);
+      const float4 o = reinterpret_cast<const float4*>(s_buf + j * kWave)[r * C + (c ^ (r & 7))];
+      sum += __builtin_amdgcn_ldexpf(s_sum[j][r], e);
+      if constexpr (WEIGH) every += __builtin_amdgcn_ldexpf(s_all[j][r], e);
+      v.x += __builtin_amdgcn_ldexpf(o.x, e);
+      v.y += __builtin_amdgcn_ldexpf(o.y, e);
+      v.z += __builtin_amdgcn_ldexpf(o.z, e);
+      v.w += __builtin_amdgcn_ldexpf(o.w, e);
+    }
+    if (w.part >= 0) {
+      float* to = g.part + w.part * kPart<D>;
+      if (c == 0) {
+        to[r] = m;
+        to[32 + r] = sum;
+        if constexpr (WEIGH) to[64 + r] = every;
+      }
+      *reinterpret_cast<float4*>(to + 96 + r * D + 4 * c) = v;
+      continue;
+    }
+    if constexpr (WEIGH) {
+      if (c == 0)
+        g.stats[((int64_t)w.b * g.kv_heads + w.hk) * 32 * g.tiles + w.r0 + r] =
+            every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const int32_t query = g.by_group.of(w.r0 + r);
+    *reinterpret_cast<u32x2*>(g.o + w.b * g.st.o[0] + query * g.st.o[1] +
+                              (w.hk * g.group + w.r0 + r - query * g.group) * g.st.o[2] + 4 * c) =
+        u32x2{wpack<DT>(v.x * inv, v.y * inv), wpack<DT>(v.z * inv, v.w * inv)};
   }
 }
 
@@ -388,8 +428,8 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t w0 = w.r0 + 32 * wave;
   const RowOf x = row_of(g, w, w0 + fr);
-  const int32_t first = w.off + min(w0, w.rows - 1) / g.group;
-  const int32_t last = w.off + min(w0 + 31, w.rows - 1) / g.group;
+  const int32_t first = w.off + g.by_group.of(min(w0, w.rows - 1));
+  const int32_t last = w.off + g.by_group.of(min(w0 + 31, w.rows - 1));
   const int32_t ptiles = (w.plen + kShKeys - 1) / kShKeys;
   const int32_t n_lo = w.n_lo, n_hi = w.n_hi;
   // tiles of which this wave's rows may see something
@@ -484,7 +524,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
       acc.o[u % ND] = wmma<DT>(va[u], pp[u / ND], acc.o[u % ND]);
 #pragma unroll
       for (int r = NE * u; r < NE * u + NE; r += 2) {
-        const float a = qexp_row<MODE, true>(s[r], g.c0, c1), z = qexp_row<MODE, true>(s[r + 1], g.c0, c1);
+        const float a = row_exp<MODE>(s[r], g.c0, c1), z = row_exp<MODE>(s[r + 1], g.c0, c1);
         const uint32_t pair = wpack<DT>(a, z);
         acc.sum = wsum<DT>(pair, acc.sum);
         if constexpr (WEIGH) all += a + z;
@@ -575,7 +615,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   for (int j = 0; j < 32 / RPL; ++j) {
     const int r = RPL * j + lane / CH, c = lane % CH;
     if (w0 + r >= w.rows) continue;
-    const int32_t qi = (w0 + r) / g.group, hd = w.hk * g.group + (w0 + r) % g.group;
+    const int32_t qi = g.by_group.of(w0 + r), hd = w.hk * g.group + w0 + r - qi * g.group;
     *reinterpret_cast<u32x4*>(g.o + w.b * g.st.o[0] + qi * g.st.o[1] + hd * g.st.o[2] + 8 * c) =
         *reinterpret_cast<const u32x4*>(ow + r * 2 * D + 16 * (c ^ kswizzle<D>(r)));
   }
@@ -594,51 +634,49 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void shared_kernel(SharedArgs g) 
   if (blockIdx.x < g.gwork) {
     w.whole = true;
     many = g.gmany != 0;
-    const uint32_t tiles = many ? ((uint32_t)g.gtiles + kShWaves - 1) / kShWaves : (uint32_t)g.gtiles;
-    uint32_t id = by_xcd(blockIdx.x, g.gwork);
-    const int32_t t32 = (int32_t)(id % tiles) * (many ? kShWaves : 1);
-    id /= tiles;
-    split = (int32_t)(id % (uint32_t)g.gsplit);
-    const uint32_t bh = id / (uint32_t)g.gsplit;
-    w.hk = (int32_t)(bh % (uint32_t)g.kv_heads);
-    w.b = (int32_t)(bh / (uint32_t)g.kv_heads) * g.members;
+    const uint32_t id = by_xcd(blockIdx.x, g.gwork), rest = g.by_gtiles.of(id);
+    const int32_t t32 = (int32_t)(id - rest * g.by_gtiles.d) * (many ? kShWaves : 1);
+    const uint32_t bh = g.by_gsplit.of(rest), grp = g.by_heads.of(bh);
+    split = (int32_t)(rest - bh * g.by_gsplit.d);
+    w.hk = (int32_t)(bh - grp * g.by_heads.d);
+    w.b = (int32_t)grp * g.members;
     w.r0 = 32 * t32;
     w.rows = g.members * g.sq * g.group;
     w.off = w.own = 0;
-    w.plen = prefix_len(g, w.b / g.members);
+    w.plen = prefix_len(g, (int32_t)grp);
     w.apart = g.gsplit;
     w.part = group_part(g, bh, t32) + split;
   } else {
     w.whole = false;
     many = g.many != 0;
     const uint32_t at = blockIdx.x - g.gwork;
-    uint32_t id;
+    uint32_t id = at;
     w.part = -1;
     w.apart = g.nsplit;
-    if (at < g.full) {
-      id = by_xcd(at, g.full);
-    } else {
-      const uint32_t cut = by_xcd(at - g.full, g.tail * (uint32_t)g.nsplit);
-      split = (int32_t)(cut % (uint32_t)g.nsplit);
-      id = cut / (uint32_t)g.nsplit;
-      w.part = own_part(g, (int64_t)id * (many ? kShWaves : 1)) + split;
-      id += g.full;
+    if (at >= g.full) {
+      // the first parts of all tiles, then the second ones: as sequences differ in length, the
+      // last parts are the ones that have nothing to do
+      const uint32_t cut = at - g.full;
+      split = (int32_t)g.by_tail.of(cut);
+      const uint32_t item = cut - (uint32_t)split * g.by_tail.d;
+      w.part = own_part(g, (int64_t)item * (many ? kShWaves : 1)) + split;
+      id = g.full + item;
     }
     const TileOf t = tile_of(g, id);
-    w.hk = (int32_t)(t.bh % (uint32_t)g.kv_heads);
-    w.b = (int32_t)(t.bh / (uint32_t)g.kv_heads);
+    w.b = (int32_t)g.by_heads.of(t.bh);
+    w.hk = (int32_t)t.bh - w.b * g.kv_heads;
     w.r0 = t.tile * (many ? 32 * kShWaves : 32);
     const int32_t qlen = seq_len(g.q_lens, w.b, g.sq);
     w.off = seq_len(g.kv_lens, w.b, g.skv) - qlen;
     w.rows = qlen * g.group;
     w.own = tile_keys(g, w.off, w.r0, w.rows);
-    w.plen = g.gsplit > 0 ? 0 : prefix_len(g, w.b / g.members);
+    w.plen = g.gsplit > 0 ? 0 : prefix_len(g, g.by_members.of(w.b));
   }
   if (w.r0 >= w.rows) return;
   w.n_lo = 0;
   w.n_hi = list_blocks(w.plen, w.own, many);
   if (w.part >= 0) {
-    const int32_t per = (w.whole ? g.gchunk : g.chunk) * (many ? 1 : 2);
+    const int32_t per = (int32_t)(w.whole ? g.by_gper.d : g.by_per.d);
     w.n_lo = split * per;
     w.n_hi = min(w.n_hi, w.n_lo + per);
     if (w.n_lo >= w.n_hi) return;
@@ -659,15 +697,14 @@ template <int D>
 __device__ __forceinline__ Parts parts_of(const SharedArgs& g, uint32_t id, uint32_t bh, int b, int32_t row,
                                           int32_t rows, int32_t off) {
   Parts p;
-  const int hk = bh % (uint32_t)g.kv_heads, grp = b / g.members;
+  const int hk = (int)bh - b * g.kv_heads, grp = g.by_members.of(b);
   const int32_t plen = prefix_len(g, grp);
   const int32_t of_group = (b - grp * g.members) * g.sq * g.group + row;
-  const int wide = g.many ? kShWaves : 1;
-  const int32_t t32 = row >> 5;
-  p.ng = g.gsplit > 0 ? list_parts(plen, 0, g.gmany != 0, g.gchunk) : 0;
+  const int32_t t32 = row >> 5, in = g.many ? t32 & (kShWaves - 1) : 0;   // in: of the workgroup's tile
+  p.ng = g.gsplit > 0 ? list_parts(plen, 0, g.gmany != 0, g.by_gper) : 0;
   p.pg = g.part + group_part(g, (int64_t)grp * g.kv_heads + hk, of_group >> 5) * kPart<D>;
-  p.po = g.part + own_part(g, (int64_t)(id - g.full) * wide + t32 % wide) * kPart<D>;
-  p.n = p.ng + list_parts(g.gsplit > 0 ? 0 : plen, tile_keys(g, off, t32 / wide * wide * 32, rows), g.many != 0, g.chunk);
+  p.po = g.part + own_part(g, (int64_t)(id - g.full) * (g.many ? kShWaves : 1) + in) * kPart<D>;
+  p.n = p.ng + list_parts(g.gsplit > 0 ? 0 : plen, tile_keys(g, off, 32 * (t32 - in), rows), g.many != 0, g.by_per);
   p.fg = of_group & 31;
   p.fo = row & 31;
   return p;
@@ -687,8 +724,7 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
   const int team = threadIdx.x / C, c = threadIdx.x % C, k = team % T;   // team k of its row
   const uint32_t n = block * R + team / T;                               // row of all that are joined
   // tiles of 128 rows from the first one that is cut; else all rows of all key heads
-  const uint32_t per = g.many ? 32 * kShWaves : (uint32_t)(g.sq * g.group);
-  const uint32_t item = n / per;
+  const uint32_t per = g.by_rows.d, item = g.by_rows.of(n);
   int32_t row = (int32_t)(n - item * per);
   uint32_t id = g.full + item, bh = item;
   bool in;
@@ -698,10 +734,10 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
     row += t.tile * (int32_t)per;
     in = item < g.tail;
   } else {
-    id = bh * (uint32_t)g.tiles + (uint32_t)(g.tiles - 1 - (row >> 5));
-    in = item * (uint32_t)g.tiles < g.tail;
+    id = number_of(g, bh, row >> 5);
+    in = item < g.heads;
   }
-  const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)(bh - (uint32_t)b * g.kv_heads);
+  const int b = (int)g.by_heads.of(bh), hk = (int)bh - b * g.kv_heads;
   const int32_t qlen = in ? seq_len(g.q_lens, b, g.sq) : 0, rows = qlen * g.group;
   const bool live = row < rows;
   float m = kNoMax, sum = 0.0f, every = 0.0f;
@@ -755,7 +791,8 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
       g.stats[(int64_t)bh * 32 * g.tiles + row] = every > 0.0f ? float2{m, 1.0f / every} : float2{0.0f, 0.0f};
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  uint16_t* orow = g.o + b * g.st.o[0] + (row / g.group) * g.st.o[1] + (hk * g.group + row % g.group) * g.st.o[2];
+  const int32_t query = g.by_group.of(row);
+  uint16_t* orow = g.o + b * g.st.o[0] + query * g.st.o[1] + (hk * g.group + row - query * g.group) * g.st.o[2];
   *reinterpret_cast<u32x2*>(orow + 4 * c) =
       u32x2{wpack<DT>(v.x * inv, v.y * inv), wpack<DT>(v.z * inv, v.w * inv)};
 }
@@ -766,7 +803,7 @@ constexpr int kScoreSlots = 1024;
 
 template <int MODE, int D>
 __device__ __forceinline__ void weigh_slots(const SharedArgs& g, uint32_t bh, int32_t j0, float* s_row) {
-  const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)(bh % (uint32_t)g.kv_heads);
+  const int b = (int)g.by_heads.of(bh), hk = (int)bh - b * g.kv_heads;
   const int32_t qlen = seq_len(g.q_lens, b, g.sq), kvlen = seq_len(g.kv_lens, b, g.skv);
   const int32_t rows = qlen * g.group, off = kvlen - qlen;
   if (j0 >= kvlen || rows == 0) return;
@@ -803,13 +840,13 @@ __device__ __forceinline__ void weigh_slots(const SharedArgs& g, uint32_t bh, in
   const float* x = g.scores + (int64_t)bh * (g.sq * g.group) * ld + j;
   float a[4] = {};
   for (int32_t r = 0; r < rows; ++r) {
-    if (off + r / g.group < j) continue;            // no part of this row's tile need be there
+    if (off + g.by_group.of(r) < j) continue;            // no part of this row's tile need be there
     const float4 s = *reinterpret_cast<const float4*>(x + r * ld);
     const float c1 = s_row[r], inv = s_row[32 + r];
-    a[0] = __builtin_fmaf(qexp_row<MODE, true>(s.x, g.c0, c1), inv, a[0]);
-    a[1] = __builtin_fmaf(qexp_row<MODE, true>(s.y, g.c0, c1), inv, a[1]);
-    a[2] = __builtin_fmaf(qexp_row<MODE, true>(s.z, g.c0, c1), inv, a[2]);
-    a[3] = __builtin_fmaf(qexp_row<MODE, true>(s.w, g.c0, c1), inv, a[3]);
+    a[0] = __builtin_fmaf(row_exp<MODE>(s.x, g.c0, c1), inv, a[0]);
+    a[1] = __builtin_fmaf(row_exp<MODE>(s.y, g.c0, c1), inv, a[1]);
+    a[2] = __builtin_fmaf(row_exp<MODE>(s.z, g.c0, c1), inv, a[2]);
+    a[3] = __builtin_fmaf(row_exp<MODE>(s.w, g.c0, c1), inv, a[3]);
   }
   float* to = g.weight + b * g.st.weight[0] + hk * g.st.weight[1] + j;
 #pragma unroll
@@ -832,11 +869,11 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs g, uint32_t
   join_rows<DT, D, WEIGH, T>(g, blockIdx.x, s_row, s_v);
 }
 
-// The weight that 128 slots gather from a chunk of the rows. A wave holds the K of 32 slots;
+// The weight that 256 slots gather from a chunk of the rows. A wave holds the K of 64 slots;
 // the rows' queries go through LDS, 64 at a time for all waves, two buffers: the scores
 // again, the exponentials against the rows' final M, times 1 / sum. A slot's rows are added
 // in a fixed order, chunks by weigh_add_kernel.
-constexpr int kWeighSlots = 32 * kShWaves, kWeighStep = 64, kWeighRows = 2048;
+constexpr int kWeighSlots = 64 * kShWaves, kWeighStep = 64, kWeighRows = 1024;
 
 template <int DT, int MODE, int D>
 __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs g, uint32_t slot_tiles,
@@ -846,11 +883,12 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
   __shared__ __attribute__((aligned(16))) char s_buf[2 * kBuf];
   const int lane = threadIdx.x & 63, fr = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t chunk = blockIdx.x % chunks, item = blockIdx.x / chunks;
-  const uint32_t bh = item / slot_tiles;
-  const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
+  // late slots see few rows: the early ones first
+  const uint32_t heads = g.heads, t_chunk = blockIdx.x / heads, bh = blockIdx.x - t_chunk * heads;
+  const uint32_t chunk = chunks - 1u - t_chunk % chunks, tile = t_chunk / chunks;
+  const int b = (int)g.by_heads.of(bh), hk = (int)bh - b * g.kv_heads;
   const int32_t qlen = seq_len(g.q_lens, b, g.sq), kvlen = seq_len(g.kv_lens, b, g.skv);
-  const int32_t first_slot = (int32_t)(item % slot_tiles) * kWeighSlots, j0 = first_slot + 32 * wave;
+  const int32_t first_slot = (int32_t)tile * kWeighSlots, j0 = first_slot + 64 * wave;
   if (first_slot >= kvlen) return;
   const int32_t off = kvlen - qlen, rows = qlen * g.group;
   // rows of this chunk that may see the first slot
@@ -858,13 +896,15 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
   const int32_t lo = max(from >= qlen ? rows : (from * g.group) & ~(kWeighStep - 1), (int32_t)chunk * kWeighRows);
   const int32_t hi = min(rows, ((int32_t)chunk + 1) * kWeighRows);
 
-  u32x4 kf[D / 16];
-  {
-    const uint16_t* kr = g.k + b * g.st.k[0] + (int64_t)min(j0 + fr, kvlen - 1) * g.kt + hk * g.st.k[2] + 8 * h;
+  u32x4 kf[2][D / 16];
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) kf[ks] = *reinterpret_cast<const u32x4*>(kr + 16 * ks);
+  for (int u = 0; u < 2; ++u) {
+    const uint16_t* kr = g.k + b * g.st.k[0] + (int64_t)min(j0 + 32 * u + fr, kvlen - 1) * g.kt + hk * g.st.k[2] + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) kf[u][ks] = *reinterpret_cast<const u32x4*>(kr + 16 * ks);
   }
-  settle(kf);
+  settle(kf[0]);
+  settle(kf[1]);
   const uint16_t* Q = g.q + b * g.st.q[0] + hk * g.group * g.st.q[2];
   const float2* stats = g.stats + (int64_t)bh * 32 * g.tiles;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
@@ -876,14 +916,14 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
     const int r = lane / CH, pc = lane % CH;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int in = kRows * wave + RPL * j + r;
-      const int32_t row = min(r0 + in, rows - 1);
-      const uint16_t* p = Q + (row / g.group) * g.st.q[1] + (row % g.group) * g.st.q[2];
+      const int32_t row = min(r0 + kRows * wave + RPL * j + r, rows - 1);
+      const int32_t query = g.by_group.of(row);
+      const uint16_t* p = Q + query * g.st.q[1] + (row - query * g.group) * g.st.q[2];
       lds_load16(lds + kRows * 2 * D * wave + 1024 * j, p + 8 * (pc ^ kswizzle<D>(RPL * j + r)));
     }
     if (wave == 0) lds_load16(lds + 2 * kWeighStep * D, reinterpret_cast<const char*>(stats + r0) + 16 * lane);
   };
-  float acc[16] = {};
+  float acc[2][16] = {};
   if (lo < hi) load(lo, 0);
   int at = 0;
   for (int32_t r0 = lo; r0 < hi; r0 += kWeighStep, at ^= 1) {
@@ -894,38 +934,48 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
 #pragma unroll
     for (int t = 0; t < kWeighStep / 32; ++t) {
       const int32_t row = r0 + 32 * t + fr;
-      f32x16 s = {};
+      f32x16 s[2] = {};
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-        s = wmma<DT>(kf[ks], read_k<D>(buf + 64 * D * t, fr, h, ks), s);
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const u32x4 qf = read_k<D>(buf + 64 * D * t, fr, h, ks);
+        s[0] = wmma<DT>(kf[0][ks], qf, s[0]);
+        s[1] = wmma<DT>(kf[1][ks], qf, s[1]);
+      }
       const float2 ms = *reinterpret_cast<const float2*>(buf + 2 * kWeighStep * D + 8 * (32 * t + fr));
       const bool in = row < hi;
       const float c1 = in ? row_c1<MODE>(ms.x) : -INFINITY, inv = in ? ms.y : 0.0f;   // e = 0 behind the rows
-      if (off + (r0 + 32 * t) / g.group < j0 + 31) hide_behind(s, j0, off + row / g.group, h);
+      const int32_t first = off + g.by_group.of(r0 + 32 * t);
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        acc[r] = __builtin_fmaf(qexp_row<MODE, true>(s[r], g.c0, c1), inv, acc[r]);
+      for (int u = 0; u < 2; ++u) {
+        if (first < j0 + 32 * u + 31) hide_behind(s[u], j0 + 32 * u, off + g.by_group.of(row), h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          acc[u][r] = __builtin_fmaf(row_exp<MODE>(s[u][r], g.c0, c1), inv, acc[u][r]);
+      }
     }
   }
-  float mine = 0.0f;                                 // lane r < 16 of a half: slot r's sum
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    float v = acc[r];
+  for (int u = 0; u < 2; ++u) {
+    float mine = 0.0f;                               // lane r < 16 of a half: slot r's sum
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) v += __shfl_xor(v, o, 64);
-    mine = fr == r ? v : mine;
+    for (int r = 0; r < 16; ++r) {
+      float v = acc[u][r];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) v += __shfl_xor(v, o, 64);
+      mine = fr == r ? v : mine;
+    }
+    const int32_t j = j0 + 32 * u + 8 * (fr >> 2) + 4 * h + (fr & 3);
+    if (fr >= 16 || j >= kvlen) continue;
+    if (chunks == 1)
+      g.weight[b * g.st.weight[0] + hk * g.st.weight[1] + j] += mine;
+    else
+      g.sums[((int64_t)bh * chunks + chunk) * g.skv + j] = mine;
   }
-  const int32_t j = j0 + 8 * (fr >> 2) + 4 * h + (fr & 3);
-  if (fr >= 16 || j >= kvlen) return;
-  if (chunks == 1)
-    g.weight[b * g.st.weight[0] + hk * g.st.weight[1] + j] += mine;
-  else
-    g.sums[((int64_t)bh * chunks + chunk) * g.skv + j] = mine;
 }
 
 __global__ __launch_bounds__(256) void weigh_add_kernel(SharedArgs g, uint32_t blocks, uint32_t chunks) {
   const uint32_t bh = blockIdx.x / blocks;
-  const int hk = bh % (uint32_t)g.kv_heads, b = bh / (uint32_t)g.kv_heads;
+  const int b = (int)g.by_heads.of(bh), hk = (int)bh - b * g.kv_heads;
   const int32_t kvlen = seq_len(g.kv_lens, b, g.skv), qlen = seq_len(g.q_lens, b, g.sq);
   const int32_t j = (int32_t)(blockIdx.x % blocks) * 256 + (int32_t)threadIdx.x;
   if (j >= kvlen) return;
@@ -964,7 +1014,22 @@ struct SharedPlan {
   bool gmany = false, many = false, stored = false;
 };
 constexpr int64_t kShSlots = 512;       // workgroups that run at once
-constexpr int64_t kManyRows = 96;
+constexpr int64_t kManyRows = 96, kBriefSteps = 16;
+
+// Steps of 64 keys a workgroup of 32 rows takes of `all`: four rounds of workgroups where
+// there is enough, as sequences differ in length; at least 512 keys, unless compute units
+// would be left without work.
+static int64_t few_chunk(int64_t all) {
+  const auto per = [&](int64_t n) { return (all + n - 1) / n; };
+  return std::max({per(4 * kShSlots), std::min<int64_t>(8, per(kShSlots / 2)), (int64_t)2});
+}
+
+// The same for 128 rows: one round; at least 1024 keys, unless most compute units would be
+// left without work (they have the sequences' own keys to read meanwhile).
+static int64_t many_chunk(int64_t all) {
+  const auto per = [&](int64_t n) { return (all + n - 1) / n; };
+  return std::max({per(kShSlots), std::min<int64_t>(16, per(kShSlots / 4)), (int64_t)4});
+}
 
 static int64_t wide_tiles(int64_t rows, bool many) { return many ? (rows + 127) / 128 : (rows + 31) / 32; }
 
@@ -979,11 +1044,13 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
   p.stored = weigh && rows <= 32;
   const int64_t psteps = (s.sp + 63) / 64;
   int64_t steps = (s.skv + 63) / 64;
-  if (s.sp > 0 && rows < kManyRows && all > rows) {
+  // few keys, which a workgroup a tile goes over in the time that a second launch takes
+  const bool brief = !p.many && (psteps + steps) * ((items + 255) / 256) <= kBriefSteps;
+  if (s.sp > 0 && rows < kManyRows && all > rows && !brief) {
     p.gtiles = (all + 31) / 32;
     p.gmany = all > 32;
     p.gitems = s.groups * s.kv_heads * wide_tiles(all, p.gmany);
-    p.gchunk = std::max<int64_t>(getenv("GMIN") ? atoi(getenv("GMIN")) : 4, (psteps * p.gitems + (getenv("GN") ? atoi(getenv("GN")) : kShSlots) - 1) / (getenv("GN") ? atoi(getenv("GN")) : kShSlots));
+    p.gchunk = p.gmany ? many_chunk(psteps * p.gitems) : few_chunk(psteps * p.gitems);
     p.gsplit = (psteps + p.gchunk - 1) / p.gchunk;
   } else {
     steps += psteps;
@@ -995,7 +1062,7 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
     p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * rest + kShSlots - 1) / kShSlots);
   } else {
     p.tail = items;
-    p.chunk = std::max<int64_t>(getenv("CMIN") ? atoi(getenv("CMIN")) : 2, (steps * items + (getenv("CN") ? atoi(getenv("CN")) : 2048) - 1) / (getenv("CN") ? atoi(getenv("CN")) : 2048));
+    p.chunk = brief ? steps : few_chunk(steps * items);
   }
   p.nsplit = std::max<int64_t>(1, (steps + p.chunk - 1) / p.chunk);
   if (p.nsplit == 1 && p.gsplit == 0 && !p.stored) p.tail = 0;   // nothing to join
@@ -1182,13 +1249,23 @@ extern "C" quake_status quake_attention_shared(
   g.groups = (int32_t)groups;
   g.gtiles = (int32_t)p.gtiles;
   g.gmany = p.gmany;
-  g.gchunk = (int32_t)p.gchunk;
   g.gsplit = (int32_t)p.gsplit;
   g.gwork = (uint32_t)(p.gitems * p.gsplit);
   g.tiles = (int32_t)p.tiles;
   g.many = p.many;
-  g.chunk = (int32_t)p.chunk;
   g.nsplit = (int32_t)p.nsplit;
+  g.by_group = Div(s.group());
+  g.by_sq = Div(sq);
+  g.by_members = Div(batch / groups);
+  g.by_heads = Div(kv_heads);
+  g.by_gtiles = Div(p.gmany ? (p.gtiles + kShWaves - 1) / kShWaves : p.gtiles);
+  g.by_gsplit = Div(p.gsplit);
+  g.by_tiles = Div(p.many ? (p.tiles + kShWaves - 1) / kShWaves : p.tiles);
+  g.by_tail = Div(p.tail);
+  g.by_gper = Div(p.gchunk * (p.gmany ? 1 : 2));
+  g.by_per = Div(p.chunk * (p.many ? 1 : 2));
+  g.by_rows = Div(p.many ? 32 * kShWaves : sq * s.group());
+  g.heads = (uint32_t)(batch * kv_heads);
   g.full = (uint32_t)p.full;
   g.tail = (uint32_t)p.tail;
   g.c0 = c0;
