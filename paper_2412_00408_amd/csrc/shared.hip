@@ -210,14 +210,22 @@ __device__ __forceinline__ void hide_behind(f32x16& s, int32_t n0, int32_t lim, 
 // times it is one multiply-add, z (a_m / 2) + 2^i. An instruction less than with the mantissa
 // joined to the exponent, and two roundings.
 template <int MODE>
-__device__ __forceinline__ float row_exp(float x, float c0, float c1) {
+__device__ __forceinline__ float q2_of_z(uint32_t z) {
+  return __builtin_fmaf(as_f(z), as_f((z & kMantMask) | 0x3F000000u), as_f(z & kSignExpMask));
+}
+// Two at a time: a wait state follows each piece of inline assembly.
+template <int MODE>
+__device__ __forceinline__ void row_exp(float x, float y, float c0, float c1, float& ex, float& ey) {
   if constexpr (MODE == Q2) {
-    uint32_t z;
-    const float l = __builtin_fmaf(x, c0, c1);
-    asm("v_cvt_u32_f32 %0, %1" : "=v"(z) : "v"(l));
-    return __builtin_fmaf(as_f(z), as_f((z & kMantMask) | 0x3F000000u), as_f(z & kSignExpMask));
+    uint32_t zx, zy;
+    asm("v_cvt_u32_f32 %0, %2\n\tv_cvt_u32_f32 %1, %3"
+        : "=&v"(zx), "=v"(zy)
+        : "v"(__builtin_fmaf(x, c0, c1)), "v"(__builtin_fmaf(y, c0, c1)));
+    ex = q2_of_z<MODE>(zx);
+    ey = q2_of_z<MODE>(zy);
   } else {
-    return qexp_row<MODE, true>(x, c0, c1);
+    ex = qexp_row<MODE, true>(x, c0, c1);
+    ey = qexp_row<MODE, true>(y, c0, c1);
   }
 }
 
@@ -328,7 +336,7 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     u32x4 pr[2];
     float e[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) e[r] = row_exp<MODE>(s[r], g.c0, c1);
+    for (int r = 0; r < 16; r += 2) row_exp<MODE>(s[r], s[r + 1], g.c0, c1, e[r], e[r + 1]);
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {                // summed as rounded: numerator and denominator
       const uint32_t pair = wpack<DT>(e[r], e[r + 1]);   // share the rounding
@@ -519,12 +527,14 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
         ka[u + 2] = get_k(KN, u + 2);
         va[u + 2] = get_v(VP, u + 2);
       }
+      // the operand that was read last first: one wait for both
       const f32x16 zero = {};
-      sn = wmma<DT>(ka[u], qf[u], u == 0 ? zero : sn);
       acc.o[u % ND] = wmma<DT>(va[u], pp[u / ND], acc.o[u % ND]);
+      sn = wmma<DT>(ka[u], qf[u], u == 0 ? zero : sn);
 #pragma unroll
       for (int r = NE * u; r < NE * u + NE; r += 2) {
-        const float a = row_exp<MODE>(s[r], g.c0, c1), z = row_exp<MODE>(s[r + 1], g.c0, c1);
+        float a, z;
+        row_exp<MODE>(s[r], s[r + 1], g.c0, c1, a, z);
         const uint32_t pair = wpack<DT>(a, z);
         acc.sum = wsum<DT>(pair, acc.sum);
         if constexpr (WEIGH) all += a + z;
@@ -843,10 +853,11 @@ __device__ __forceinline__ void weigh_slots(const SharedArgs& g, uint32_t bh, in
     if (off + g.by_group.of(r) < j) continue;            // no part of this row's tile need be there
     const float4 s = *reinterpret_cast<const float4*>(x + r * ld);
     const float c1 = s_row[r], inv = s_row[32 + r];
-    a[0] = __builtin_fmaf(row_exp<MODE>(s.x, g.c0, c1), inv, a[0]);
-    a[1] = __builtin_fmaf(row_exp<MODE>(s.y, g.c0, c1), inv, a[1]);
-    a[2] = __builtin_fmaf(row_exp<MODE>(s.z, g.c0, c1), inv, a[2]);
-    a[3] = __builtin_fmaf(row_exp<MODE>(s.w, g.c0, c1), inv, a[3]);
+    float e[4];
+    row_exp<MODE>(s.x, s.y, g.c0, c1, e[0], e[1]);
+    row_exp<MODE>(s.z, s.w, g.c0, c1, e[2], e[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __builtin_fmaf(e[i], inv, a[i]);
   }
   float* to = g.weight + b * g.st.weight[0] + hk * g.st.weight[1] + j;
 #pragma unroll
@@ -949,8 +960,12 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
       for (int u = 0; u < 2; ++u) {
         if (first < j0 + 32 * u + 31) hide_behind(s[u], j0 + 32 * u, off + g.by_group.of(row), h);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          acc[u][r] = __builtin_fmaf(row_exp<MODE>(s[u][r], g.c0, c1), inv, acc[u][r]);
+        for (int r = 0; r < 16; r += 2) {
+          float a, z;
+          row_exp<MODE>(s[u][r], s[u][r + 1], g.c0, c1, a, z);
+          acc[u][r] = __builtin_fmaf(a, inv, acc[u][r]);
+          acc[u][r + 1] = __builtin_fmaf(z, inv, acc[u][r + 1]);
+        }
       }
     }
   }
