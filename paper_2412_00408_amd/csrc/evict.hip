@@ -54,7 +54,7 @@ constexpr int kBins = 2048, kHeld = 16, kEach = 8;
 template <int THREADS>
 struct ChooseShared {
   uint32_t bins[3][kBins];
-  uint32_t wave[THREADS / 64], equal[THREADS / 64], found[2];
+  uint32_t wave[THREADS / 64], equal[THREADS / 64], found[3];
 };
 
 template <int THREADS, bool HELD>
@@ -119,6 +119,7 @@ __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w,
         if (above < left && left <= above + c[i]) {
           sh.found[0] = (uint32_t)(top - i);
           sh.found[1] = above;
+          sh.found[2] = c[i];
         }
         above += c[i];
       }
@@ -126,10 +127,13 @@ __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w,
     __syncthreads();
     key |= sh.found[0] << shift;
     left -= sh.found[1];
+    if (left < sh.found[2] || key == 0) return false;
+    --key;                                           // all of these fit: what is above them and they
+    left = 0;
+    return true;
   };
-  digit(sh.bins[0], 21, 0x7FFu, 0u);
-  digit(sh.bins[1], 10, 0x7FFu, 0xFFE00000u);
-  digit(sh.bins[2], 0, 0x3FFu, 0xFFFFFC00u);
+  if (!digit(sh.bins[0], 21, 0x7FFu, 0u) && !digit(sh.bins[1], 10, 0x7FFu, 0xFFE00000u))
+    digit(sh.bins[2], 0, 0x3FFu, 0xFFFFFC00u);
   // kept slots in order: those above the key and, of its equals, the first `left`
   uint32_t n = 0, ne = 0;
   each([&](int32_t, uint32_t k) {

@@ -440,6 +440,8 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   const int32_t last = w.off + g.by_group.of(min(w0 + 31, w.rows - 1));
   const int32_t ptiles = (w.plen + kShKeys - 1) / kShKeys;
   const int32_t n_lo = w.n_lo, n_hi = w.n_hi;
+  // blocks of 32 of the prefix, and of the own keys, that all rows of this wave see
+  const int32_t pseen = w.plen >> 5, oseen = 2 * ptiles + (first < 0 ? 0 : (first + 1) >> 5);
   // tiles of which this wave's rows may see something
   const int32_t seen = w.whole || last < 0 ? 0 : last / kShKeys + 1;
   const int32_t t_hi = __any(x.live) ? min(n_hi, ptiles + seen) : n_lo;
@@ -449,13 +451,55 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
   const Lists lists(g, w);
   const uint32_t lds = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf + wave * kRows * 2 * D);
-  auto load_k = [&](int32_t t, uint32_t at) {
+  // Whole tiles of the longer list go from a running base and this lane's own offsets, which
+  // leaves two scalar instructions a load; the others as any run of keys.
+  const bool main_p = w.plen >= w.own;
+  const int32_t whole_lo = main_p ? 0 : ptiles, whole_hi = whole_lo + (main_p ? w.plen : w.own) / kShKeys;
+  constexpr int RPL = 512 / D, NL = kRows / RPL;   // rows a load, loads of K or V of a tile
+  uint32_t koff[NL], voff[NL];
+  const uint32_t ktok = 2u * (uint32_t)(main_p ? g.pkt : g.kt), vtok = 2u * (uint32_t)(main_p ? g.pvt : g.vt);
+  {
+    constexpr int CH = D / 8;
+    const int r = lane / CH, pc = lane % CH;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const uint32_t in = kRows * wave + RPL * j + r;
+      koff[j] = in * ktok + 16u * (uint32_t)(pc ^ kswizzle<D>(RPL * j + r));
+      voff[j] = in * vtok + 16u * (uint32_t)(pc ^ vswizzle<D>(RPL * j + r));
+    }
+  }
+  const int64_t kstep = (int64_t)kShKeys * ktok, vstep = (int64_t)kShKeys * vtok;
+  const char* kcur = scalar_base((const char*)(main_p ? lists.pk : lists.k) + (n_lo - whole_lo) * kstep);
+  const char* vcur = scalar_base((const char*)(main_p ? lists.pv : lists.v) + (n_lo - whole_lo) * vstep);
+  auto any_k = [&](int32_t t, uint32_t at) {
     stage_list<D, false, kRows>(lds + kTile * at, g, w, lists, t < ptiles,
                                 kShKeys * (t < ptiles ? t : t - ptiles) + kRows * wave, lane);
   };
+  // tiles one after the other from n_lo on
+  auto load_k = [&](int32_t t) {
+    const uint32_t at = (uint32_t)(t - n_lo) & 1u;
+    if (t >= whole_lo && t < whole_hi) {
+      uint32_t to = lds + kTile * at;
+      asm volatile("" : "+s"(to));
+#pragma unroll
+      for (int j = 0; j < NL; ++j) lds_load16(to + 1024 * j, koff[j], kcur);
+    } else {
+      any_k(t, at);
+    }
+    kcur += kstep;
+  };
   auto load_v = [&](int32_t t) {
-    stage_list<D, true, kRows>(lds + kTile * (2 + ((t - n_lo) & 1)), g, w, lists, t < ptiles,
-                               kShKeys * (t < ptiles ? t : t - ptiles) + kRows * wave, lane);
+    const uint32_t at = 2u + ((uint32_t)(t - n_lo) & 1u);
+    if (t >= whole_lo && t < whole_hi) {
+      uint32_t to = lds + kTile * at;
+      asm volatile("" : "+s"(to));
+#pragma unroll
+      for (int j = 0; j < NL; ++j) lds_load16(to + 1024 * j, voff[j], vcur);
+    } else {
+      stage_list<D, true, kRows>(lds + kTile * at, g, w, lists, t < ptiles,
+                                 kShKeys * (t < ptiles ? t : t - ptiles) + kRows * wave, lane);
+    }
+    vcur += vstep;
   };
 
   RowAcc<D> acc;
@@ -507,9 +551,10 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
       ka[u] = get_k(KN, u);
       va[u] = get_v(VP, u);
     }
-    const bool p = n < 2 * ptiles;
-    const int32_t n0 = 32 * (p ? n : n - 2 * ptiles);
-    if (n0 + 31 > (p ? w.plen - 1 : first)) hide_behind(s, n0, p ? w.plen - 1 : x.pos, h);
+    if (n >= (n < 2 * ptiles ? pseen : oseen)) {     // not all keys are seen by all rows
+      const bool p = n < 2 * ptiles;
+      hide_behind(s, 32 * (p ? n : n - 2 * ptiles), p ? w.plen - 1 : x.pos, h);
+    }
     float top = s[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
@@ -559,7 +604,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
     wait_lds();
     wait_loads<0>();
     __syncthreads();
-    if (t + 2 < n_hi) load_k(t + 2, (t - n_lo) & 1);
+    if (t + 2 < n_hi) load_k(t + 2);
     if (t + 1 < n_hi) load_v(t + 1);
     if (!mine) return;
     step(2 * t + 1, std::integral_constant<int, 2 - B>{}, std::integral_constant<int, B>{}, sb, sa, pa, pb);
@@ -570,10 +615,10 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
     }
   };
   if (n_lo < n_hi) {
-    load_k(n_lo, 3);   // V of the tile before the first is read (times 0): K's rows, finite where K is
-    load_k(n_lo, 0);
+    any_k(n_lo, 3);    // V of the tile before the first is read (times 0): K's rows, finite where K is
+    load_k(n_lo);
     load_v(n_lo);
-    if (n_lo + 1 < n_hi) load_k(n_lo + 1, 1);
+    if (n_lo + 1 < n_hi) load_k(n_lo + 1);
     wait_loads<0>();
     __syncthreads();
   }
@@ -620,7 +665,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
     }
   __builtin_amdgcn_wave_barrier();
   wait_lds();
-  constexpr int CH = D / 8, RPL = 64 / CH;
+  constexpr int CH = D / 8;
 #pragma unroll
   for (int j = 0; j < 32 / RPL; ++j) {
     const int r = RPL * j + lane / CH, c = lane % CH;
@@ -920,17 +965,33 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void weigh_rows_kernel(SharedArgs
   const float2* stats = g.stats + (int64_t)bh * 32 * g.tiles;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_buf);
-  // queries r0 on to buffer `at`: this wave's kRows of them, chunks swizzled as K's
+  // Queries r0 on to buffer `at`: this wave's kRows of them, chunks swizzled as K's. Where
+  // whole queries make up a step and lie close, from a running base and this lane's own
+  // offsets.
+  const bool near = kWeighStep % g.group == 0 && (g.sq == 1 || g.st.q[1] <= (1 << 23)) &&
+                    (g.group == 1 || g.st.q[2] <= (1 << 23));
+  const int lr = lane / CH, pc = lane % CH;
+  uint32_t qoff[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int32_t in = kRows * wave + RPL * j + lr, query = g.by_group.of(in);
+    qoff[j] = 2u * ((uint32_t)query * (uint32_t)g.st.q[1] + (uint32_t)(in - query * g.group) * (uint32_t)g.st.q[2]) +
+              16u * (uint32_t)(pc ^ kswizzle<D>(RPL * j + lr));
+  }
   auto load = [&](int32_t r0, int at) {
     uint32_t lds = lds0 + kBuf * at;
     asm volatile("" : "+s"(lds));
-    const int r = lane / CH, pc = lane % CH;
+    if (near && r0 + kWeighStep <= rows) {
+      const char* base = scalar_base(Q + (int64_t)g.by_group.of(r0) * g.st.q[1]);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int32_t row = min(r0 + kRows * wave + RPL * j + r, rows - 1);
-      const int32_t query = g.by_group.of(row);
-      const uint16_t* p = Q + query * g.st.q[1] + (row - query * g.group) * g.st.q[2];
-      lds_load16(lds + kRows * 2 * D * wave + 1024 * j, p + 8 * (pc ^ kswizzle<D>(RPL * j + r)));
+      for (int j = 0; j < N; ++j) lds_load16(lds + kRows * 2 * D * wave + 1024 * j, qoff[j], base);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int32_t row = min(r0 + kRows * wave + RPL * j + lr, rows - 1), query = g.by_group.of(row);
+        const uint16_t* p = Q + query * g.st.q[1] + (row - query * g.group) * g.st.q[2];
+        lds_load16(lds + kRows * 2 * D * wave + 1024 * j, p + 8 * (pc ^ kswizzle<D>(RPL * j + lr)));
+      }
     }
     if (wave == 0) lds_load16(lds + 2 * kWeighStep * D, reinterpret_cast<const char*>(stats + r0) + 16 * lane);
   };
