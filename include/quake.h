@@ -461,11 +461,11 @@ quake_status quake_attention_window(const void* q, const void* k, const void* v,
  *          one (NULL) every sequence reads the prefix for itself; a weight needs one. It
  *          lies outside the bytes from the first to the last of every operand. Calls that may
  *          run at the same time need workspaces of their own.
- *   batch a multiple of groups; batch, sq <= 2^24, sp + skv <= 2^30, heads <= 2^16, fewer
- *   than 2^24 tiles of 32 rows of one key head (a row: one query of one head) and, with a
- *   weight, of 128 slots of one key head; fewer than 2^30 rows of a group and key head; dtype
- *   QUAKE_BF16 or QUAKE_F16 (else QUAKE_EDTYPE); t as in quake_attention. batch == 0 or
- *   sq == 0 launches nothing.
+ *   batch a multiple of groups; batch, sq <= 2^24, sp + skv <= 2^30, heads <= 2^16, at
+ *   most 2^30 rows of a group and key head (a row: one query of one head), fewer than 2^24
+ *   tiles of 32 rows of one sequence and key head and, with a weight, of 256 slots by 1024
+ *   rows; dtype QUAKE_BF16 or QUAKE_F16 (else QUAKE_EDTYPE); t as in quake_attention.
+ *   batch == 0 or sq == 0 launches nothing.
  * The same call gives the same bits every time (with a workspace others than without). A
  * visible key or value that is not finite may spoil the outputs of other queries that share
  * it, those that do not see it among them.

@@ -303,14 +303,9 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
   }
   u32x4 qf[D / 16];
   load_q<D>(g, x, h, qf);
-  bool stored = false;
   for (int32_t n = n_lo + wave; n < n_hi; n += kShWaves) {
     const bool more = n + kShWaves < n_hi;
-    // K is here; the scores of the block before and V may be on their way
-    if (stored)
-      wait_loads<kLoads + 4>();
-    else
-      wait_loads<kLoads>();
+    wait_loads<kLoads>();                           // K is here, V may be on its way
     f32x16 s = {};
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) s = wmma<DT>(read_k<D>(buf, fr, h, ks), qf[ks], s);
@@ -319,14 +314,6 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
     const bool p = n < pblocks;
     const int32_t n0 = 32 * (p ? n : n - pblocks);
     if (n0 + 31 > (p ? w.plen - 1 : first)) hide_behind(s, n0, p ? w.plen - 1 : x.pos, h);
-    if constexpr (WEIGH) {
-      stored = g.scores != nullptr && !p;
-      if (stored && x.live) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<float4*>(scores + n0 + 8 * i) = float4{s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]};
-      }
-    }
     const float top = block_top<MODE>(s, g.c0);
     if (__any(top > acc.m + (kLift<DT> + kLazy))) {
       const int32_t e = raise_max<DT>(top, acc);
@@ -344,13 +331,18 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
       pr[r >> 3][(r >> 1) & 3] = pair;
     }
     if constexpr (WEIGH) all += sum16(e);
-    // V is here; the next K and the scores may be on their way
-    if (!more)
-      wait_loads<0>();
-    else if (stored)
-      wait_loads<kLoads + 4>();
+    if (more)
+      wait_loads<kLoads>();                         // V is here, the next K may be on its way
     else
-      wait_loads<kLoads>();
+      wait_loads<0>();
+    if constexpr (WEIGH) {
+      // between the loads of K and V, whose number the waits go by
+      if (scores != nullptr && !p && x.live) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(scores + n0 + 8 * i) = float4{s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]};
+      }
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -1138,7 +1130,7 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
     p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * rest + kShSlots - 1) / kShSlots);
   } else {
     p.tail = items;
-    p.chunk = brief ? steps : few_chunk(steps * items);
+    p.chunk = brief ? std::max<int64_t>(steps, 1) : few_chunk(steps * items);
   }
   p.nsplit = std::max<int64_t>(1, (steps + p.chunk - 1) / p.chunk);
   if (p.nsplit == 1 && p.gsplit == 0 && !p.stored) p.tail = 0;   // nothing to join
@@ -1164,7 +1156,7 @@ static SharedSpace shared_space(const SharedShape& s, const SharedPlan& p, bool 
   const int64_t heads = s.batch * s.kv_heads;
   const int64_t n = s.groups * s.kv_heads * p.gtiles * p.gsplit + p.tail * (p.many ? kShWaves : 1) * p.nsplit;
   if (p.gsplit > 0 || p.tail > 0) x.part = n * (96 + 32 * s.dim) * 4;
-  if (!weigh) return x;
+  if (!weigh || heads * s.sq == 0) return x;
   if (p.stored) {
     x.scores = heads * s.sq * s.group() * score_row(s.skv) * 4;
   } else {
@@ -1230,8 +1222,9 @@ extern "C" quake_status quake_attention_shared_workspace_size(int64_t batch, int
                                                               int64_t kv_heads, int64_t dim, int weigh,
                                                               int64_t* bytes) {
   const SharedShape s{batch, groups, sq, sp, skv, heads, kv_heads, dim};
-  if (bytes == nullptr || !shared_shape_ok(s) || (weigh && !weigh_shape_ok(s))) return QUAKE_EINVAL;
-  *bytes = shared_space(s, shared_plan(s, weigh != 0, true), weigh != 0).total();
+  const bool weighs = weigh != 0 && skv > 0;
+  if (bytes == nullptr || !shared_shape_ok(s) || (weighs && !weigh_shape_ok(s))) return QUAKE_EINVAL;
+  *bytes = shared_space(s, shared_plan(s, weighs, true), weighs).total();
   return QUAKE_OK;
 }
 
@@ -1269,7 +1262,7 @@ extern "C" quake_status quake_attention_shared(
     }
   }
   if (!rows_apart(st.o, nq, 3, dim)) return QUAKE_EINVAL;
-  const bool weigh = weight != nullptr;
+  const bool weigh = weight != nullptr && skv > 0;
   const int64_t nw[2] = {batch, kv_heads};
   const int64_t* sw = st.weight;
   if (weigh) {
@@ -1302,7 +1295,7 @@ extern "C" quake_status quake_attention_shared(
   g.k = static_cast<const uint16_t*>(k);
   g.v = static_cast<const uint16_t*>(v);
   g.o = static_cast<uint16_t*>(o);
-  g.weight = weight;
+  g.weight = weigh ? weight : nullptr;
   g.prefix_lens = prefix_lens;
   g.q_lens = q_lens;
   g.kv_lens = kv_lens;

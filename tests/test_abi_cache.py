@@ -66,6 +66,20 @@ def test_shared_weight_refusals(q):
             q._size("quake_attention_shared_workspace_size", *size)
 
 
+def test_shared_workspace_sizes(q):
+    name = "quake_attention_shared_workspace_size"
+    for weigh in (0, 1):
+        assert q._size(name, 0, 1, 1, 0, 8, 4, 4, 64, weigh) == 0
+        assert q._size(name, 2, 1, 0, 100, 8, 4, 4, 64, weigh) == 0
+        assert q._size(name, 2, 1, 1, 0, 0, 4, 4, 64, weigh) == 0          # no keys at all
+        assert q._size(name, 2, 1, 200, 0, 0, 4, 4, 64, weigh) == 0
+        assert q._size(name, 1, 1, 1, 5, 0, 4, 4, 64, weigh) == 0
+        for size in ((64, 1, 1, 8192, 1024, 32, 8, 128), (5, 5, 7, 300, 0, 8, 1, 64), (1, 1, 1, 1 << 20, 9, 128, 1, 128),
+                     (1 << 20, 1, 1, 64, 64, 1, 1, 64), (3, 1, 500, 1, 500, 7, 7, 64), (1, 1, 1, 1 << 29, 1 << 29, 1, 1, 64)):
+            assert q._size(name, *size, weigh) % 16 == 0
+    assert q._size(name, 4, 1, 1, 500, 64, 8, 2, 64, 0) == 0               # brief: no second launch
+
+
 def test_shared_formats_modes_and_empty_calls(q):
     call = shared(q)
     assert call(dt=0) == q.EDTYPE and call(dt=7) == q.EDTYPE and call(mode=4) == q.EMODE

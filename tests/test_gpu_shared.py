@@ -147,6 +147,14 @@ def test_rows_without_keys(q):
     for ws in (None, q.attention_shared_workspace(none[0], none[1][:, :0], none[3])):
         o = q.quake_attention_shared(none[0], none[1][:, :0], none[2][:, :0], *none[3:], workspace=ws)
         check("no slots", o, None, want)
+    w = torch.zeros((2, 2, 0), device="cuda")                    # nor any weight
+    o = q.quake_attention_shared(none[0], none[1][:, :0], none[2][:, :0], *none[3:], weight=w)
+    check("no slots, a weight", o, None, want)
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")     # no keys at all
+    for sq in (3, 300):
+        y = torch.randn((2, sq, 4, 64), device="cuda").to(torch.bfloat16)
+        o = q.quake_attention_shared(y, none[1][:, :0], none[2][:, :0], weight=w, workspace=ws)
+        assert (o == 0).all()
 
 
 def test_scores_that_keep_rising_and_extreme_scores(q):
