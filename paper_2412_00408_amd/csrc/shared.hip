@@ -1109,11 +1109,11 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
   const int64_t items = s.batch * s.kv_heads * wide_tiles(rows, p.many);
   p.full = items;
   if (!workspace || items == 0 || items >= (1 << 18)) return p;   // 32 rows a tile are joined in one launch
-  p.stored = weigh && rows <= 32;
   const int64_t psteps = (s.sp + 63) / 64;
   int64_t steps = (s.skv + 63) / 64;
   // few keys, which a workgroup a tile goes over in the time that a second launch takes
   const bool brief = !p.many && (psteps + steps) * ((items + 255) / 256) <= kBriefSteps;
+  p.stored = weigh && rows <= 32 && !(brief && items <= 64);
   if (s.sp > 0 && rows < kManyRows && all > rows && !brief) {
     p.gtiles = (all + 31) / 32;
     p.gmany = all > 32;
