@@ -46,10 +46,10 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 // A workgroup a sequence and key head; a wave has a run of the slots. The key of the last one
 // that fits comes digit by digit from the top (11, 11 and 10 bits), by counting in LDS those
-// whose upper digits are the key's. Up to kHeld slots a thread stay in registers, longer rows
-// are read again for each digit and twice for the result. One compute unit's instructions
+// whose upper digits are the key's. Up to kHeldLong slots a thread stay in registers, longer
+// rows are read again for each digit and twice for the result. One compute unit's instructions
 // and barriers bound it.
-constexpr int kBins = 2048, kHeld = 16, kEach = 8;
+constexpr int kBins = 2048, kHeld = 16, kHeldLong = 40, kEach = 8;
 
 template <int THREADS>
 struct ChooseShared {
@@ -57,10 +57,10 @@ struct ChooseShared {
   uint32_t wave[THREADS / 64], equal[THREADS / 64], found[3];
 };
 
-template <int THREADS, bool HELD>
+template <int THREADS, int HELD>     // HELD: slots a thread holds, 0: reads them again
 __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w, int32_t len, int32_t* kept,
                                              ChooseShared<THREADS>& sh) {
-  constexpr int E = HELD ? kHeld : kEach, W = THREADS / 64, N = kBins / THREADS;   // bins a thread
+  constexpr int E = HELD > 0 ? HELD : kEach, W = THREADS / 64, N = kBins / THREADS;   // bins a thread
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t lo = g.sinks, hi = len - g.recent;
@@ -68,27 +68,32 @@ __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w,
   const int32_t from = wave * run, to = min(from + run, len);
   uint32_t u[E];
   const auto fetch = [&](int32_t i0) {
-    float x[E];
+    constexpr int F = E < 16 ? E : 16;               // loads in flight
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int32_t i = i0 + 64 * e + lane;
-      x[e] = i < to ? w[i] : 0.0f;
-    }
+    for (int e0 = 0; e0 < E; e0 += F) {
+      float x[F];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int32_t i = i0 + 64 * e + lane;
-      u[e] = i >= to ? kNever : i < lo || i >= hi ? kAlways : weight_key(x[e]);
+      for (int e = 0; e < F; ++e) {
+        const int32_t i = i0 + 64 * (e0 + e) + lane;
+        x[e] = i < to ? w[i] : 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < F; ++e) {
+        const int32_t i = i0 + 64 * (e0 + e) + lane;
+        u[e0 + e] = i >= to ? kNever : i < lo || i >= hi ? kAlways : weight_key(x[e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   const auto each = [&](auto f) {      // f(slot of lane 0, this lane's key), of this wave's run
     for (int32_t i0 = from; i0 < to; i0 += 64 * E) {
-      if (!HELD) fetch(i0);
+      if (HELD == 0) fetch(i0);
 #pragma unroll
       for (int e = 0; e < E; ++e)
         if (i0 + 64 * e < to) f(i0 + 64 * e, u[e]);
     }
   };
-  if (HELD) fetch(from);
+  if (HELD > 0) fetch(from);
   for (int i = threadIdx.x; i < 3 * kBins; i += THREADS) sh.bins[0][i] = 0;
   __syncthreads();
   uint32_t key = 0, left = (uint32_t)g.budget;       // of the slots whose upper digits are key's
@@ -175,98 +180,130 @@ __global__ __launch_bounds__(THREADS) void evict_choose_kernel(EvictArgs g) {
   }
   const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
   if (len <= kHeld * THREADS)
-    choose_slots<THREADS, true>(g, w, len, kept, sh);
+    choose_slots<THREADS, kHeld>(g, w, len, kept, sh);
+  else if (THREADS == 1024 && len <= kHeldLong * THREADS)
+    choose_slots<THREADS, THREADS == 1024 ? kHeldLong : 0>(g, w, len, kept, sh);
   else
-    choose_slots<THREADS, false>(g, w, len, kept, sh);
+    choose_slots<THREADS, 0>(g, w, len, kept, sh);
 }
 
-// The weights of a key head, and the sequence's length.
-constexpr int kMvEach = 4;
+constexpr int kMvEach = 4, kCopyEach = 8;
 
-template <int THREADS>
-__device__ __forceinline__ void move_weights(const EvictArgs& g, int b, int hk, const int32_t* kept) {
-  const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
-  float* wo = g.wo + b * g.st.weight_out[0] + hk * g.st.weight_out[1];
-  int32_t n = 0;                                     // kept
-  for (int32_t i0 = 0; i0 < g.budget; i0 += THREADS * kMvEach) {
+// How many of kept[0 .. n) there are (the rest is -1 and behind them), by one wave.
+__device__ __forceinline__ int32_t count_kept(const int32_t* kept, int32_t n) {
+  const int lane = threadIdx.x & 63;
+  int32_t lo = 0, hi = n;                            // kept[lo - 1] is one, kept[hi] is none
+  while (lo < hi) {
+    const int32_t step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const int32_t m = (int32_t)__popcll(__ballot(i < hi && kept[min(i, n - 1)] >= 0));
+    // probes 0 .. m - 1 are there, probe m is not
+    const int32_t top = lo + m * step;
+    lo = m == 0 ? lo : lo + (m - 1) * step + 1;
+    hi = m == 0 ? lo : min(hi, top);
+  }
+  return lo;
+}
+__device__ __forceinline__ void put_length(const EvictArgs& g, int b, int hk, const int32_t* kept) {
+  if (hk > 0 || g.lens_out == nullptr || threadIdx.x >= 64) return;
+  const int32_t n = count_kept(kept, g.budget);
+  if (threadIdx.x == 0) g.lens_out[b] = n;
+}
+
+// Weights [i, end) of a key head's kept slots; IN: in place, as shift_rows.
+template <int THREADS, bool IN>
+__device__ __forceinline__ void move_weights(const EvictArgs& g, const float* w, float* wo, const int32_t* kept,
+                                             int32_t i, int32_t end) {
+  for (; i < end; i += THREADS * kMvEach) {
     float x[kMvEach];
     int32_t from[kMvEach];
 #pragma unroll
     for (int j = 0; j < kMvEach; ++j) {
-      const int32_t i = i0 + j * THREADS + (int32_t)threadIdx.x;
-      from[j] = i < g.budget ? kept[i] : -1;
+      const int32_t k = i + j * THREADS + (int32_t)threadIdx.x;
+      from[j] = k < end ? kept[k] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kMvEach; ++j) x[j] = from[j] >= 0 ? w[from[j]] : 0.0f;
+    if (IN) {
+#pragma unroll
+      for (int j = 0; j < kMvEach; ++j) asm volatile("" : "+v"(x[j]));
+      __syncthreads();
     }
 #pragma unroll
     for (int j = 0; j < kMvEach; ++j) {
-      x[j] = from[j] >= 0 ? w[from[j]] : 0.0f;
-      n += from[j] >= 0;
+      const int32_t k = i + j * THREADS + (int32_t)threadIdx.x;
+      if (k < end) wo[k] = x[j];
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kMvEach; ++j) {
-      const int32_t i = i0 + j * THREADS + (int32_t)threadIdx.x;
-      if (i < g.budget) wo[i] = x[j];
-    }
-  }
-  for (int32_t i = g.budget + (int32_t)threadIdx.x; i < g.slots; i += THREADS) wo[i] = 0.0f;
-  if (hk > 0 || g.lens_out == nullptr) return;
-  __shared__ int32_t s_n[THREADS / 64];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
-  if ((threadIdx.x & 63) == 0) s_n[threadIdx.x >> 6] = n;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < THREADS / 64; ++i) n += s_n[i];
-    g.lens_out[b] = n;
   }
 }
 
-// Rows [i, end) of a slice of K or V of one key head; IN: in place, a round's rows are all read
-// before one is written, and the next round's are on their way meanwhile.
-template <int THREADS, int EACH, bool IN>
-__device__ __forceinline__ void move_rows(const EvictArgs& g, const char* src, char* dst, int64_t ss, int64_t sd,
-                                          const int32_t* kept, int32_t i, int32_t end, uint32_t c0, uint32_t width) {
-  const uint32_t rows = THREADS / width;             // at a time; the last threads may have none
-  const uint32_t r = threadIdx.x / width, c = threadIdx.x - r * width;
-  const bool has = r < rows;
-  src += 16 * (int64_t)(c0 + c);
-  dst += 16 * (int64_t)(c0 + c);
-  struct Round {
-    int32_t from[EACH];
-    u32x4 x[EACH];
-  };
-  const auto read = [&](Round& q, int32_t at) {
+// Rows [i, end) of a slice of K or V of one key head: a thread's chunk of a row, kMvEach rows
+// at a time.
+struct RowsOf {
+  uint32_t rows, r, c;      // rows at a time (the last threads may have none), this thread's
+  __device__ __forceinline__ RowsOf(uint32_t threads, uint32_t width) {
+    rows = threads / width;
+    r = threadIdx.x / width;
+    c = threadIdx.x - r * width;
+  }
+};
+template <int THREADS>
+__device__ __forceinline__ void copy_rows(const char* src, char* dst, int64_t ss, int64_t sd, const int32_t* kept,
+                                          int32_t i, int32_t end, uint32_t c0, uint32_t width) {
+  const RowsOf t(THREADS, width);
+  src += 16 * (int64_t)(c0 + t.c);
+  dst += 16 * (int64_t)(c0 + t.c);
+  const int32_t any = kept[0];                       // what is read in the place of none
+  if (t.r >= t.rows || any < 0) return;              // a cache may have no slot at all
+  for (int32_t k0 = i + (int32_t)t.r; k0 < end; k0 += (int32_t)(kCopyEach * t.rows)) {
+    int32_t from[kCopyEach];
+    u32x4 x[kCopyEach];
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      const int32_t k = at + (int32_t)(j * rows + r);
-      q.from[j] = has && k < end ? kept[k] : -1;
-      if (IN && q.from[j] == k) q.from[j] = -1;      // stays where it is
+    for (int j = 0; j < kCopyEach; ++j) from[j] = kept[min(k0 + (int32_t)(j * t.rows), end - 1)];
+#pragma unroll
+    for (int j = 0; j < kCopyEach; ++j)
+      x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (from[j] < 0 ? any : from[j]) * ss));
+#pragma unroll
+    for (int j = 0; j < kCopyEach; ++j) {
+      const int32_t k = k0 + (int32_t)(j * t.rows);
+      if (k < end && from[j] >= 0) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4*>(dst + k * sd));
+    }
+  }
+}
+// In place: a round's rows are all read before one is written, and the next round's are on
+// their way meanwhile.
+template <int THREADS>
+__device__ __forceinline__ void shift_rows(char* at, int64_t stride, const int32_t* kept, int32_t end, uint32_t c0,
+                                           uint32_t width) {
+  const RowsOf t(THREADS, width);
+  at += 16 * (int64_t)(c0 + t.c);
+  int32_t from[kMvEach], next[kMvEach];
+  u32x4 x[kMvEach], y[kMvEach];
+  const int32_t step = (int32_t)(kMvEach * t.rows);
+  const auto read = [&](int32_t k0, int32_t (&f)[kMvEach], u32x4 (&v)[kMvEach]) {
+#pragma unroll
+    for (int j = 0; j < kMvEach; ++j) {
+      const int32_t k = k0 + (int32_t)(j * t.rows + t.r);
+      f[j] = t.r < t.rows && k < end ? kept[k] : -1;
+      if (f[j] == k) f[j] = -1;                      // stays where it is
     }
 #pragma unroll
-    for (int j = 0; j < EACH; ++j)
-      if (q.from[j] >= 0) q.x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + q.from[j] * ss));
+    for (int j = 0; j < kMvEach; ++j)
+      v[j] = f[j] >= 0 ? *reinterpret_cast<const u32x4*>(at + f[j] * stride) : u32x4{0u, 0u, 0u, 0u};
   };
-  const auto write = [&](const Round& q, int32_t at) {
+  read(0, from, x);
+  for (int32_t k0 = 0; k0 < end; k0 += step) {
+    read(k0 + step, next, y);
+    // this round's are in registers, in every wave
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      const int32_t k = at + (int32_t)(j * rows + r);
-      if (q.from[j] >= 0) __builtin_nontemporal_store(q.x[j], reinterpret_cast<u32x4*>(dst + k * sd));
-    }
-  };
-  const int32_t step = (int32_t)(EACH * rows);
-  Round a;
-  read(a, i);
-  for (; i < end; i += step) {
-    Round next;
-    read(next, i + step);
-    if (IN) {
-      // this round's reads are in registers, in every wave
+    for (int j = 0; j < kMvEach; ++j) asm volatile("" : "+v"(x[j]));
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < EACH; ++j) asm volatile("" : "+v"(a.x[j]));
-      __syncthreads();
+    for (int j = 0; j < kMvEach; ++j) {
+      if (from[j] >= 0)
+        *reinterpret_cast<u32x4*>(at + (int64_t)(k0 + (int32_t)(j * t.rows + t.r)) * stride) = x[j];
+      from[j] = next[j];
+      x[j] = y[j];
     }
-    write(a, i);
-    a = next;
   }
 }
 
@@ -278,37 +315,42 @@ __global__ __launch_bounds__(kInThreads) void evict_shift_kernel(EvictArgs g) {
   const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)bh - b * g.kv_heads;
   const int32_t* kept = g.kept + (int64_t)bh * g.budget;
   if (part == parts - 1u) {
-    move_weights<kInThreads>(g, b, hk, kept);
+    float* w = g.wo + b * g.st.weight_out[0] + hk * g.st.weight_out[1];
+    put_length(g, b, hk, kept);
+    move_weights<kInThreads, true>(g, w, w, kept, 0, g.budget);
+    for (int32_t i = g.budget + (int32_t)threadIdx.x; i < g.slots; i += kInThreads) w[i] = 0.0f;
     return;
   }
   const bool value = part >= (uint32_t)g.slices;
   const uint32_t c0 = (part - (value ? (uint32_t)g.slices : 0u)) * (uint32_t)g.slice;
-  const int64_t* st = value ? g.st.v : g.st.k;
-  char* at = (value ? g.vo : g.ko) + b * st[0] + hk * st[2];
-  move_rows<kInThreads, kMvEach, true>(g, at, at, st[1], st[1], kept, 0, g.budget, c0,
-                                       min((uint32_t)g.slice, (uint32_t)g.row16 - c0));
+  const auto pick = [&](int64_t of_k, int64_t of_v) { return value ? of_v : of_k; };
+  char* at = (value ? g.vo : g.ko) + b * pick(g.st.k[0], g.st.v[0]) + hk * pick(g.st.k[2], g.st.v[2]);
+  shift_rows<kInThreads>(at, pick(g.st.k[1], g.st.v[1]), kept, g.budget, c0, min((uint32_t)g.slice, (uint32_t)g.row16 - c0));
 }
 
-// Into another cache: runs of g.run rows of K, of V, and the weights.
+// Into another cache: runs of g.slice rows of K, with their weights, and of V.
 constexpr int kCopyThreads = 256;
 __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictArgs g) {
-  const uint32_t parts = 2u * (uint32_t)g.slices + 1u;
+  const uint32_t parts = 2u * (uint32_t)g.slices;
   const uint32_t bh = blockIdx.x / parts, part = blockIdx.x - bh * parts;
   const int b = (int)(bh / (uint32_t)g.kv_heads), hk = (int)bh - b * g.kv_heads;
   const int32_t* kept = g.kept + (int64_t)bh * g.budget;
-  if (part == parts - 1u) {
-    move_weights<kCopyThreads>(g, b, hk, kept);
-    return;
-  }
   const bool value = part >= (uint32_t)g.slices;
-  const int32_t i = (int32_t)(part - (value ? (uint32_t)g.slices : 0u)) * g.slice;
-  const int64_t* si = value ? g.st.v : g.st.k;
-  const int64_t* so = value ? g.st.v_out : g.st.k_out;
-  const char* src = (value ? g.v : g.k) + b * si[0] + hk * si[2];
-  char* dst = (value ? g.vo : g.ko) + b * so[0] + hk * so[2];
+  const int32_t i = (int32_t)(part - (value ? (uint32_t)g.slices : 0u)) * g.slice, end = min(i + g.slice, g.budget);
+  const auto pick = [&](int64_t of_k, int64_t of_v) { return value ? of_v : of_k; };
+  const char* src = (value ? g.v : g.k) + b * pick(g.st.k[0], g.st.v[0]) + hk * pick(g.st.k[2], g.st.v[2]);
+  char* dst = (value ? g.vo : g.ko) + b * pick(g.st.k_out[0], g.st.v_out[0]) + hk * pick(g.st.k_out[2], g.st.v_out[2]);
   for (uint32_t c0 = 0; c0 < (uint32_t)g.row16; c0 += kCopyThreads)
-    move_rows<kCopyThreads, kMvEach, false>(g, src, dst, si[1], so[1], kept, i, min(i + g.slice, g.budget), c0,
-                                            min((uint32_t)g.row16 - c0, (uint32_t)kCopyThreads));
+    copy_rows<kCopyThreads>(src, dst, pick(g.st.k[1], g.st.v[1]), pick(g.st.k_out[1], g.st.v_out[1]), kept, i, end, c0, min((uint32_t)g.row16 - c0, (uint32_t)kCopyThreads));
+  if (!value) {
+    const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
+    float* wo = g.wo + b * g.st.weight_out[0] + hk * g.st.weight_out[1];
+    move_weights<kCopyThreads, false>(g, w, wo, kept, i, end);
+    if (i == 0) {
+      put_length(g, b, hk, kept);
+      for (int32_t j = g.budget + (int32_t)threadIdx.x; j < g.slots; j += kCopyThreads) wo[j] = 0.0f;
+    }
+  }
 }
 
 }  // namespace qk
@@ -434,7 +476,7 @@ extern "C" quake_status quake_cache_evict(const void* k, const void* v, const fl
     rows = std::max(rows, budget * heads / (1 << 22) + 1);       // a launch takes fewer than 2^32 threads
     g.slice = (int32_t)std::min(rows, budget);
     g.slices = (int32_t)((budget + g.slice - 1) / g.slice);
-    hipLaunchKernelGGL(evict_copy_kernel, dim3((uint32_t)(heads * (2 * g.slices + 1))), dim3(kCopyThreads), 0, s, g);
+    hipLaunchKernelGGL(evict_copy_kernel, dim3((uint32_t)(heads * 2 * g.slices)), dim3(kCopyThreads), 0, s, g);
   }
   return launch_status();
 }
