@@ -264,7 +264,13 @@ __device__ __forceinline__ void stage_list(uint32_t lds, const SharedArgs& g, co
 }
 
 // 32 rows in one workgroup; the waves take every fourth block of the keys and join at the
-// end. K's next block is on its way while V of this one is used, and the other way round.
+// end. K's next block is on its way while V of this one is used, and the other way round: one
+// buffer of each a wave, so that two workgroups fit a compute unit. What bounds it is reading
+// the keys: one token for each of 32 caches of 4096 (32 heads over 8, head dim 128, bf16) 100
+// us, 5.3 TB/s; of 256 caches of 512 93 us, 5.8 TB/s; a single one of 8192 keys is bound by
+// the latency of its blocks, about 2 us each, and so are the last workgroups of a batch of
+// different lengths (32 x 4096, 267 MB: 65 us, 4.1 TB/s).
+// The scores kept for the weights cost 8 us of 126 where each of 32 caches has 4096 keys.
 template <int DT, int MODE, int D, bool WEIGH>
 __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, char* s_buf, float* s_row) {
   constexpr int kBlk = 64 * D;                      // bytes of a block of 32 rows
@@ -419,7 +425,12 @@ __device__ __forceinline__ void few_rows(const SharedArgs& g, const Work& w, cha
 // 128 rows in one workgroup, 32 a wave, which share tiles of 64 keys in LDS (two blocks of
 // 32; two tiles each of K and V), in the software pipeline of window_many_kernel: while
 // block n's scores become probabilities, the scores of block n + 1 and the second product
-// of block n - 1 are computed; one barrier a tile, between its blocks.
+// of block n - 1 are computed; one barrier a tile, between its blocks. 256 sequences
+// of 32 heads over 8 x 32768 shared keys (head dim 128, bf16): 147 us without the join, 0.93
+// PFLOP/s; 120 us, 1.15, where all operands are 0: power and its clock. By the counters
+// products take 42 % of the cycles; a wave waits 26 % of its time for memory or a barrier and
+// 32 % to issue; of about 220 instructions a wave and block 123 are VALU ones, 16 products, 42
+// scalar.
 template <int DT, int MODE, int D, bool WEIGH>
 __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, char* s_buf) {
   constexpr int kTile = 2 * kShKeys * D;            // bytes of K or V of a tile
@@ -762,7 +773,8 @@ __device__ __forceinline__ const float* part_at(const Parts& p, int32_t i, int32
   return i < p.ng ? p.pg + (int64_t)i * kPart<D> : p.po + (int64_t)(i - p.ng) * kPart<D>;
 }
 
-// Joins the parts of a row: T teams of D / 4 lanes, a lane for every four dims, which take
+// Joins the parts of a row (2048 rows of 10 parts 6 us, 8192 of 9 11 us: the latency of the
+// lengths, then the parts): T teams of D / 4 lanes, a lane for every four dims, which take
 // every T-th part with several loads in flight; then the teams' results in LDS. The order
 // is fixed.
 template <int DT, int D, bool WEIGH, int T>
@@ -844,8 +856,13 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
       u32x2{wpack<DT>(v.x * inv, v.y * inv), wpack<DT>(v.z * inv, v.w * inv)};
 }
 
-// The weight of kWeighSlots slots of a key head whose rows are one tile of 32: the scores
-// that the tiles left, against the rows' final M, which is joined here from the parts.
+// The weight of kScoreSlots slots of a key head whose rows are one tile of 32: the scores
+// that the tiles left, against the rows' final M, which is joined here from the parts. Reading
+// 4 bytes a row and key again costs less than the key once more: 32 caches of 4096 keys, head
+// dim 128, groups of 4, against weigh_rows_kernel: 1 token 127 / 199 us, 4 tokens 156 / 208, 8
+// (32 rows) 195 / 216; 16 x 4096 at head dim 64 with 1 row 69 / 124, 32 rows 134 / 134. Where
+// 64 workgroups at most go over at most 1024 keys the second launch is dearer (26 / 23 us for
+// 2 caches of 1000 keys and 32 rows), and the rows do it there.
 constexpr int kScoreSlots = 1024;
 
 template <int MODE, int D>
@@ -920,7 +937,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs g, uint32_t
 // The weight that 256 slots gather from a chunk of the rows. A wave holds the K of 64 slots;
 // the rows' queries go through LDS, 64 at a time for all waves, two buffers: the scores
 // again, the exponentials against the rows' final M, times 1 / sum. A slot's rows are added
-// in a fixed order, chunks by weigh_add_kernel.
+// in a fixed order, chunks by weigh_add_kernel. VALU issue bounds it: a prompt of 4096 tokens
+// (32 heads over 8, head dim 128, bf16) 132 us beside the 163 of its attention.
 constexpr int kWeighSlots = 64 * kShWaves, kWeighStep = 64, kWeighRows = 1024;
 
 template <int DT, int MODE, int D>
@@ -1082,18 +1100,26 @@ struct SharedPlan {
   bool gmany = false, many = false, stored = false;
 };
 constexpr int64_t kShSlots = 512;       // workgroups that run at once
+// From kManyRows rows on, 128 rows share a workgroup. Up to kBriefSteps steps a compute unit,
+// a workgroup a tile goes over all keys and nothing is joined: 4 to 16 sequences, 8 key heads, a
+// prefix of 1000 keys 13 to 14 us against 15 with rows of groups and a join, of 2000 21 to 22
+// against 16; 64 sequences: 500 keys 14 / 17, 1000 20 / 18.
 constexpr int64_t kManyRows = 96, kBriefSteps = 16;
 
 // Steps of 64 keys a workgroup of 32 rows takes of `all`: four rounds of workgroups where
 // there is enough, as sequences differ in length; at least 512 keys, unless compute units
-// would be left without work.
+// would be left without work. (32 caches of up to 4096: 256 keys each 78 us, 512 70, 1024 70,
+// 4096 69; with weights 85, 80, 83, 88. 64 over 8192 shared and up to 1024 own keys: 128 own
+// keys a workgroup 65 us, 256 57, 512 55, 1024 55.)
 static int64_t few_chunk(int64_t all) {
   const auto per = [&](int64_t n) { return (all + n - 1) / n; };
   return std::max({per(4 * kShSlots), std::min<int64_t>(8, per(kShSlots / 2)), (int64_t)2});
 }
 
 // The same for 128 rows: one round; at least 1024 keys, unless most compute units would be
-// left without work (they have the sequences' own keys to read meanwhile).
+// left without work (they have the sequences' own keys to read meanwhile). 64 over 8192 shared
+// keys: 256 keys a workgroup 74 us, 512 62, 1024 55, 1536 58; 16 x 5 tokens over 10007: 512
+// keys 48 us, 1024 43, 1280 39, 2048 48.
 static int64_t many_chunk(int64_t all) {
   const auto per = [&](int64_t n) { return (all + n - 1) / n; };
   return std::max({per(kShSlots), std::min<int64_t>(16, per(kShSlots / 4)), (int64_t)4});
@@ -1124,10 +1150,11 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
     steps += psteps;
   }
   if (p.many) {
-    // whole rounds of workgroups that each take all keys of a tile; the rest is cut up
-    const int64_t rest = items % kShSlots;
-    p.tail = rest <= 400 ? rest : 0;
-    p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * rest + kShSlots - 1) / kShSlots);
+    // Tiles that leave workgroups idle are cut up: a prompt of 600 tokens behind 4096 shared keys
+    // (152 tiles) 64 us, uncut 87; two of 900 behind 2000 (464 tiles) 93 either way, as are 8 of
+    // 600 (1216 tiles, 355 us) with the last round's tiles cut or not.
+    p.tail = items <= kShSlots * 3 / 4 ? items : 0;
+    p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * items + kShSlots - 1) / kShSlots);
   } else {
     p.tail = items;
     p.chunk = brief ? std::max<int64_t>(steps, 1) : few_chunk(steps * items);
