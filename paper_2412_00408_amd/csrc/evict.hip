@@ -294,7 +294,7 @@ __device__ __forceinline__ void shift_rows(char* at, int64_t stride, const int32
   read(0, from, x);
   for (int32_t k0 = 0; k0 < end; k0 += step) {
     read(k0 + step, next, y);
-    // this round's are in registers, in every wave
+    // these are in registers, in every wave
 #pragma unroll
     for (int j = 0; j < kMvEach; ++j) asm volatile("" : "+v"(x[j]));
     __syncthreads();
