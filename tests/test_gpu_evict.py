@@ -147,6 +147,27 @@ def test_offsets_past_32_bits(q):
     both(q, "far apart", k, v, x[2], 20, 1, 5, None)
 
 
+def test_very_many_rows(q):
+    b, hk = 1 << 18, 4
+    k, v, w = cache(b, 12, hk, 8, torch.bfloat16, 11, "ties")
+    lens = torch.randint(0, 13, (b,), dtype=torch.int32, device="cuda")
+    out = [torch.zeros((b, 8, hk, 8), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    out += [torch.zeros((b, hk, 8), device="cuda"), torch.zeros(b, dtype=torch.int32, device="cuda")]
+    kept, evicted = q.quake_cache_evict(k, v, w, 6, 1, 2, kv_lens=lens, out=out)
+    torch.cuda.synchronize()
+    for at in (slice(0, 40), slice(b // 2, b // 2 + 40), slice(b - 40, b)):
+        zero = [torch.zeros_like(a[at]) for a in out[:3]]
+        want = ref.evict(k[at], v[at], w[at], 6, 1, 2, lens[at], *zero)
+        same("many rows %s" % at, [a[at] for a in out] + [kept[at], evicted[at]], want)
+    part = slice(b - 40, b)
+    want = ref.evict(k[part], v[part], w[part], 6, 1, 2, lens[part], k[part], v[part], w[part])
+    kept, evicted = q.quake_cache_evict(k, v, w, 6, 1, 2, kv_lens=lens)
+    same("many rows in place", [a[part] for a in (k, v, w, lens, kept, evicted)], want)
+    with pytest.raises(q.QuakeError):                # 2^20 rows are the most
+        y = torch.empty((1 << 18, 1, 5, 8), dtype=torch.bfloat16, device="cuda")
+        q.quake_cache_evict(y, y.clone(), torch.empty((1 << 18, 5, 1), device="cuda"), 1)
+
+
 def test_no_slots_and_no_sequences(q):
     e = torch.empty((2, 0, 1, 64), dtype=torch.bfloat16, device="cuda")
     out = [torch.ones((2, 8, 1, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]

@@ -221,6 +221,20 @@ def test_long_prefix_and_long_cache(q):
     check("100000 own keys", q.quake_attention_shared(*x, weight=w, t=0.08, workspace=ws), w, want)
 
 
+def test_very_many_sequences(q):
+    # more tiles than are joined in one launch: every sequence reads the prefix for itself
+    b = 70000
+    for sq, weigh in ((1, True), (1, False), (9, True)):
+        x = make(b, 1, sq, 20, 10, 8, 4, 64, torch.bfloat16, 12)
+        w = weights(x) if weigh else None
+        w0 = w.clone() if weigh else None
+        ws = q.attention_shared_workspace(x[0], x[1], x[3], weigh=weigh)
+        o = q.quake_attention_shared(*x, weight=w, workspace=ws)
+        for at in (slice(0, 3), slice(b // 2, b // 2 + 3), slice(b - 3, b)):
+            want = ref.shared_attention(x[0][at], x[1][at], x[2][at], x[3], x[4], weight=w0[at] if weigh else None)
+            check("many sequences %s %s %s" % (sq, weigh, at), o[at], w[at] if weigh else None, want)
+
+
 def test_agrees_with_windowed_attention(q):
     # no prefix: the windowed operator with a window of the whole length; and a prefix is
     # what the same keys in front of every sequence's own would be
