@@ -69,19 +69,20 @@ __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w,
   const int32_t from = wave * run, to = min(from + run, len);
   uint32_t u[E];
   const auto fetch = [&](int32_t i0) {
-    constexpr int F = E < 16 ? E : 16;               // loads in flight
+    constexpr int F = E < 16 ? E : 16;               // loads in flight; the last ones may be fewer
 #pragma unroll
     for (int e0 = 0; e0 < E; e0 += F) {
+      const int end = e0 + F < E ? e0 + F : E;
       float x[F];
 #pragma unroll
-      for (int e = 0; e < F; ++e) {
-        const int32_t i = i0 + 64 * (e0 + e) + lane;
-        x[e] = i < to ? w[i] : 0.0f;
+      for (int e = e0; e < end; ++e) {
+        const int32_t i = i0 + 64 * e + lane;
+        x[e - e0] = i < to ? w[i] : 0.0f;
       }
 #pragma unroll
-      for (int e = 0; e < F; ++e) {
-        const int32_t i = i0 + 64 * (e0 + e) + lane;
-        u[e0 + e] = i >= to ? kNever : i < lo || i >= hi ? kAlways : weight_key(x[e]);
+      for (int e = e0; e < end; ++e) {
+        const int32_t i = i0 + 64 * e + lane;
+        u[e] = i >= to ? kNever : i < lo || i >= hi ? kAlways : weight_key(x[e - e0]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
