@@ -533,7 +533,7 @@ def quake_attention_shared(q, k, v, prefix_k=None, prefix_v=None, o=None, weight
         _apart(weight, "weight", ((o, "o"), (q, "q"), (k, "k"), (v, "v"), (prefix_k, "prefix_k"),
                                   (prefix_v, "prefix_v"), (prefix_lens, "prefix_lens"),
                                   (q_lens, "q_lens"), (kv_lens, "kv_lens")))
-        if workspace is None and skv:
+        if workspace is None and batch and sq and skv:   # else nothing is launched or weighed
             raise ValueError("a weight needs a workspace (attention_shared_workspace with weigh=True)")
     pl = _per_row(prefix_lens, "prefix_lens", dev, groups, torch.int32)
     ql = _per_row(q_lens, "q_lens", dev, batch, torch.int32)
