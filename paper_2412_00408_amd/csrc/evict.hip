@@ -54,7 +54,7 @@ constexpr int kBins = 2048, kHeld = 16, kHeldLong = 40, kEach = 8;
 
 template <int THREADS>
 struct ChooseShared {
-  uint32_t bins[3][kBins];
+  uint32_t bins[3 * kBins];                          // of a digit each
   uint32_t wave[THREADS / 64], equal[THREADS / 64], found[3];
 };
 
@@ -96,7 +96,7 @@ __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w,
     }
   };
   if (HELD > 0) fetch(from);
-  for (int i = threadIdx.x; i < 3 * kBins; i += THREADS) sh.bins[0][i] = 0;
+  for (int i = threadIdx.x; i < 3 * kBins; i += THREADS) sh.bins[i] = 0;
   __syncthreads();
   uint32_t key = 0, left = (uint32_t)g.budget;       // of the slots whose upper digits are key's
   const auto digit = [&](uint32_t* bins, int shift, uint32_t mask, uint32_t upper) {
@@ -139,8 +139,8 @@ __device__ __forceinline__ void choose_slots(const EvictArgs& g, const float* w,
     left = 0;
     return true;
   };
-  if (!digit(sh.bins[0], 21, 0x7FFu, 0u) && !digit(sh.bins[1], 10, 0x7FFu, 0xFFE00000u))
-    digit(sh.bins[2], 0, 0x3FFu, 0xFFFFFC00u);
+  if (!digit(sh.bins, 21, 0x7FFu, 0u) && !digit(sh.bins + kBins, 10, 0x7FFu, 0xFFE00000u))
+    digit(sh.bins + 2 * kBins, 0, 0x3FFu, 0xFFFFFC00u);
   // kept slots in order: those above the key and, of its equals, the first `left`
   uint32_t n = 0, ne = 0;
   each([&](int32_t, uint32_t k) {

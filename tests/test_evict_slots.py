@@ -1,7 +1,8 @@
-"""Which slots a thread of evict.hip's choice holds, on the CPU under AddressSanitizer and
-UndefinedBehaviorSanitizer (g++): the text of the loop that fills them, taken from the
-source, runs lane by lane for rows on both sides of every limit. It has to fill all of
-the thread's slots, with the keys that they should have, and nothing behind them."""
+"""Loops of evict.hip's choice, taken from the source, on the CPU under AddressSanitizer
+and UndefinedBehaviorSanitizer (g++), thread by thread. The one that holds a thread's slots,
+for rows on both sides of every limit: it has to fill all of them, with the keys that they
+should have, and nothing behind them. The one that clears the counts: it has to reach
+all of them and stay within each array."""
 import os
 import re
 import shutil
@@ -73,20 +74,71 @@ def _taken(pattern, text):
     return found[0]
 
 
-@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
-def test_held_slots_stay_in_bounds(tmp_path):
+CLEAR = r"""
+#include <cstdint>
+#include <cstdio>
+#include <cstring>
+%(sizes)s
+%(shared)s
+static struct { int x; } threadIdx;
+template <int THREADS>
+static bool check() {
+  static ChooseShared<THREADS> sh;
+  std::memset((void*)&sh, 0xFF, sizeof sh);
+  for (threadIdx.x = 0; threadIdx.x < THREADS; ++threadIdx.x) {
+%(clear)s
+  }
+  for (int i = 0; i < 3; ++i) {
+    static uint32_t none[kBins];
+    if (std::memcmp((const char*)&sh.bins + 4 * kBins * i, none, sizeof none) != 0) return false;
+  }
+  return sh.wave[0] == 0xFFFFFFFFu && sh.found[2] == 0xFFFFFFFFu;
+}
+int main() {
+  if (check<256>() && check<1024>()) std::printf("all clear\n");
+}
+"""
+
+
+def _source():
     with open(os.path.join(build.CSRC, "evict.hip")) as f:
-        text = f.read()
-    parts = dict(keys=_taken(r"^constexpr uint32_t kAlways.*?^}$", text),
-                 sizes=_taken(r"^constexpr int kBins[^;]*;", text),
-                 fetch=_taken(r"^  const auto fetch = .*?^  };$", text))
-    assert "weight_key" in parts["keys"]
-    src, exe = str(tmp_path / "held.cpp"), str(tmp_path / "held")
+        return f.read()
+
+
+def _taken(pattern, text):
+    found = re.findall(pattern, text, re.S | re.M)
+    assert len(found) == 1, pattern
+    return found[0]
+
+
+def _runs(tmp_path, code, says):
+    src, exe = str(tmp_path / "taken.cpp"), str(tmp_path / "taken")
     with open(src, "w") as f:
-        f.write(HARNESS % parts)
+        f.write(code)
     r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", *SAN, src, "-o", exe], capture_output=True, text=True)
     if r.returncode != 0 and "asan" in r.stderr.lower():
         pytest.skip("sanitizer runtime not available: " + r.stderr[-300:])
     assert r.returncode == 0, r.stderr[-3000:]
     run = subprocess.run([exe], capture_output=True, text=True, timeout=300)
-    assert run.returncode == 0 and "all held" in run.stdout, run.stdout[-600:] + run.stderr[-2000:]
+    assert run.returncode == 0 and says in run.stdout, run.stdout[-600:] + run.stderr[-2000:]
+
+
+needs_gxx = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+SIZES = r"^constexpr int kBins[^;]*;"
+
+
+@needs_gxx
+def test_held_slots_stay_in_bounds(tmp_path):
+    text = _source()
+    parts = dict(keys=_taken(r"^constexpr uint32_t kAlways.*?^}$", text), sizes=_taken(SIZES, text),
+                 fetch=_taken(r"^  const auto fetch = .*?^  };$", text))
+    assert "weight_key" in parts["keys"]
+    _runs(tmp_path, HARNESS % parts, "all held")
+
+
+@needs_gxx
+def test_cleared_counts_stay_in_bounds(tmp_path):
+    text = _source()
+    parts = dict(sizes=_taken(SIZES, text), shared=_taken(r"^template <int THREADS>\nstruct ChooseShared.*?^};$", text),
+                 clear=_taken(r"fetch\(from\);\n(.*?)  __syncthreads", text))
+    _runs(tmp_path, CLEAR % parts, "all clear")
