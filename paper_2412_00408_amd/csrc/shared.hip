@@ -1144,7 +1144,7 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
     p.gtiles = (all + 31) / 32;
     p.gmany = all > 32;
     p.gitems = s.groups * s.kv_heads * wide_tiles(all, p.gmany);
-    p.gchunk = p.gmany ? many_chunk(psteps * p.gitems) : few_chunk(psteps * p.gitems);
+    p.gchunk = std::min(p.gmany ? many_chunk(psteps * p.gitems) : few_chunk(psteps * p.gitems), psteps);
     p.gsplit = (psteps + p.gchunk - 1) / p.gchunk;
   } else {
     steps += psteps;
@@ -1157,8 +1157,9 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
     p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * items + kShSlots - 1) / kShSlots);
   } else {
     p.tail = items;
-    p.chunk = brief ? std::max<int64_t>(steps, 1) : few_chunk(steps * items);
+    p.chunk = brief ? steps : few_chunk(steps * items);
   }
+  p.chunk = std::max<int64_t>(1, std::min(p.chunk, steps));   // the kernels divide by 31-bit numbers
   p.nsplit = std::max<int64_t>(1, (steps + p.chunk - 1) / p.chunk);
   if (p.nsplit == 1 && p.gsplit == 0 && !p.stored) p.tail = 0;   // nothing to join
   if (p.tail == 0) p.nsplit = 1;
