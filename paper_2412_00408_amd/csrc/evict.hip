@@ -181,12 +181,14 @@ __global__ __launch_bounds__(THREADS) void evict_choose_kernel(EvictArgs g) {
     return;
   }
   const float* w = g.weight + b * g.st.weight[0] + hk * g.st.weight[1];
-  if (len <= kHeld * THREADS)
+  if (THREADS == 256 || len <= kHeld * THREADS) {    // 256 threads are launched for no longer rows
     choose_slots<THREADS, kHeld>(g, w, len, kept, sh);
-  else if (THREADS == 1024 && len <= kHeldLong * THREADS)
-    choose_slots<THREADS, THREADS == 1024 ? kHeldLong : 0>(g, w, len, kept, sh);
-  else
-    choose_slots<THREADS, 0>(g, w, len, kept, sh);
+  } else if constexpr (THREADS > 256) {
+    if (len <= kHeldLong * THREADS)
+      choose_slots<THREADS, kHeldLong>(g, w, len, kept, sh);
+    else
+      choose_slots<THREADS, 0>(g, w, len, kept, sh);
+  }
 }
 
 constexpr int kMvEach = 4, kCopyEach = 8;
