@@ -54,12 +54,12 @@ struct SharedArgs {
   int32_t pkt, pvt, kt, vt;                     // token strides
   int32_t groups, sq, sp, skv, group, kv_heads, members;
   int32_t gtiles, gmany, gsplit;                // of a group's rows (gsplit 0: none) ..
-  int32_t tiles, many, nsplit;                  // .. and a sequence's: tiles of 32 rows, whether 128
-                                                // rows share a workgroup, the most parts of a tile
-  uint32_t heads, gwork, full, tail;            // key heads of all sequences; workgroups of groups' rows; tiles that
-                                                // one workgroup takes, and those cut into parts
+  int32_t tiles, many, cut, nsplit;             // .. and a sequence's: tiles of 32 rows, whether 128 rows
+                                                // share a workgroup, whether tiles are cut into parts, the most of one
+  uint32_t heads, gwork, items;                 // key heads of all sequences; workgroups of groups' rows; the
+                                                // sequences' tiles in units of one workgroup's
   Div by_group, by_sq, by_members, by_heads;    // heads: key heads
-  Div by_gtiles, by_gsplit, by_tiles, by_tail;     // tiles: in units of one workgroup's
+  Div by_gtiles, by_gsplit, by_tiles, by_items;    // tiles: in units of one workgroup's
   Div by_gper, by_per, by_rows;                 // blocks of a part; rows of a key head or, many, 128
   float c0;                                     // 2^23 t / ln2 (EXACT: t / ln2)
 };
@@ -94,8 +94,7 @@ __device__ __forceinline__ int32_t tile_keys(const SharedArgs& g, int32_t off, i
 __device__ __forceinline__ int32_t prefix_len(const SharedArgs& g, int32_t group) {
   return g.sp == 0 ? 0 : seq_len(g.prefix_lens, group, g.sp);
 }
-// The first part of a tile: a group's; a sequence's, whose tiles are counted from the first
-// one that is cut.
+// The first part of a tile: a group's; a sequence's, the tiles numbered as they are launched.
 __device__ __forceinline__ int64_t group_part(const SharedArgs& g, int64_t bh, int32_t tile) {
   return (bh * g.gtiles + tile) * g.gsplit;
 }
@@ -680,8 +679,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& g, const Work& w, ch
 }
 
 // The groups' rows against the prefixes, then each sequence's against its own keys (where no
-// rows of groups are formed: against the prefix first), the tiles that one workgroup takes
-// before those that are cut into parts.
+// rows of groups are formed: against the prefix first), whole or cut into parts.
 template <int DT, int MODE, int D, bool WEIGH>
 __global__ __launch_bounds__(64 * kShWaves, 2) void shared_kernel(SharedArgs g) {
   __shared__ __attribute__((aligned(16))) char s_buf[4 * 2 * kShKeys * D];
@@ -711,14 +709,12 @@ __global__ __launch_bounds__(64 * kShWaves, 2) void shared_kernel(SharedArgs g) 
     uint32_t id = at;
     w.part = -1;
     w.apart = g.nsplit;
-    if (at >= g.full) {
+    if (g.cut) {
       // the first parts of all tiles, then the second ones: as sequences differ in length, the
       // last parts are the ones that have nothing to do
-      const uint32_t cut = at - g.full;
-      split = (int32_t)g.by_tail.of(cut);
-      const uint32_t item = cut - (uint32_t)split * g.by_tail.d;
-      w.part = own_part(g, (int64_t)item * (many ? kShWaves : 1)) + split;
-      id = g.full + item;
+      split = (int32_t)g.by_items.of(at);
+      id = at - (uint32_t)split * g.items;
+      w.part = own_part(g, (int64_t)id * (many ? kShWaves : 1)) + split;
     }
     const TileOf t = tile_of(g, id);
     w.b = (int32_t)g.by_heads.of(t.bh);
@@ -761,7 +757,7 @@ __device__ __forceinline__ Parts parts_of(const SharedArgs& g, uint32_t id, uint
   const int32_t t32 = row >> 5, in = g.many ? t32 & (kShWaves - 1) : 0;   // in: of the workgroup's tile
   p.ng = g.gsplit > 0 ? list_parts(plen, 0, g.gmany != 0, g.by_gper) : 0;
   p.pg = g.part + group_part(g, (int64_t)grp * g.kv_heads + hk, of_group >> 5) * kPart<D>;
-  p.po = g.part + own_part(g, (int64_t)(id - g.full) * (g.many ? kShWaves : 1) + in) * kPart<D>;
+  p.po = g.part + own_part(g, (int64_t)id * (g.many ? kShWaves : 1) + in) * kPart<D>;
   p.n = p.ng + list_parts(g.gsplit > 0 ? 0 : plen, tile_keys(g, off, 32 * (t32 - in), rows), g.many != 0, g.by_per);
   p.fg = of_group & 31;
   p.fo = row & 31;
@@ -782,16 +778,16 @@ __device__ __forceinline__ void join_rows(const SharedArgs& g, uint32_t block, f
   constexpr int C = D / 4, TEAMS = 256 / C, R = TEAMS / T, U = 4;
   const int team = threadIdx.x / C, c = threadIdx.x % C, k = team % T;   // team k of its row
   const uint32_t n = block * R + team / T;                               // row of all that are joined
-  // tiles of 128 rows from the first one that is cut; else all rows of all key heads
+  // all tiles of 128 rows; else all rows of all key heads
   const uint32_t per = g.by_rows.d, item = g.by_rows.of(n);
   int32_t row = (int32_t)(n - item * per);
-  uint32_t id = g.full + item, bh = item;
+  uint32_t id = item, bh = item;
   bool in;
   if (g.many) {
     const TileOf t = tile_of(g, id);
     bh = t.bh;
     row += t.tile * (int32_t)per;
-    in = item < g.tail;
+    in = item < g.items;
   } else {
     id = number_of(g, bh, row >> 5);
     in = item < g.heads;
@@ -1096,8 +1092,8 @@ static bool shared_shape_ok(const SharedShape& s) {
 // few: the prefix is then read once for all, and its scores are full tiles.
 struct SharedPlan {
   int64_t gtiles = 0, gchunk = 1, gsplit = 0, gitems = 0;   // items: tiles of a workgroup
-  int64_t tiles = 0, chunk = 1, nsplit = 1, full = 0, tail = 0;
-  bool gmany = false, many = false, stored = false;
+  int64_t tiles = 0, chunk = 1, nsplit = 1, items = 0;
+  bool gmany = false, many = false, cut = false, stored = false;
 };
 constexpr int64_t kShSlots = 512;       // workgroups that run at once
 // From kManyRows rows on, 128 rows share a workgroup. Up to kBriefSteps steps a compute unit,
@@ -1132,8 +1128,7 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
   const int64_t rows = s.sq * s.group(), all = rows * (s.batch / s.groups);
   p.tiles = (rows + 31) / 32;
   p.many = rows >= kManyRows;
-  const int64_t items = s.batch * s.kv_heads * wide_tiles(rows, p.many);
-  p.full = items;
+  const int64_t items = p.items = s.batch * s.kv_heads * wide_tiles(rows, p.many);
   if (!workspace || items == 0 || items >= (1 << 18)) return p;   // 32 rows a tile are joined in one launch
   const int64_t psteps = (s.sp + 63) / 64;
   int64_t steps = (s.skv + 63) / 64;
@@ -1153,17 +1148,16 @@ static SharedPlan shared_plan(const SharedShape& s, bool weigh, bool workspace) 
     // Tiles that leave workgroups idle are cut up: a prompt of 600 tokens behind 4096 shared keys
     // (152 tiles) 64 us, uncut 87; two of 900 behind 2000 (464 tiles) 93 either way, as are 8 of
     // 600 (1216 tiles, 355 us) with the last round's tiles cut or not.
-    p.tail = items <= kShSlots * 3 / 4 ? items : 0;
-    p.chunk = p.tail == 0 ? 1 : std::max<int64_t>(8, (steps * items + kShSlots - 1) / kShSlots);
+    p.cut = items <= kShSlots * 3 / 4;
+    p.chunk = !p.cut ? 1 : std::max<int64_t>(8, (steps * items + kShSlots - 1) / kShSlots);
   } else {
-    p.tail = items;
+    p.cut = true;
     p.chunk = brief ? steps : few_chunk(steps * items);
   }
   p.chunk = std::max<int64_t>(1, std::min(p.chunk, steps));   // the kernels divide by 31-bit numbers
   p.nsplit = std::max<int64_t>(1, (steps + p.chunk - 1) / p.chunk);
-  if (p.nsplit == 1 && p.gsplit == 0 && !p.stored) p.tail = 0;   // nothing to join
-  if (p.tail == 0) p.nsplit = 1;
-  p.full = items - p.tail;
+  if (p.nsplit == 1 && p.gsplit == 0 && !p.stored) p.cut = false;   // nothing to join
+  if (!p.cut) p.nsplit = 1;
   return p;
 }
 
@@ -1182,8 +1176,8 @@ struct SharedSpace {
 static SharedSpace shared_space(const SharedShape& s, const SharedPlan& p, bool weigh) {
   SharedSpace x{};
   const int64_t heads = s.batch * s.kv_heads;
-  const int64_t n = s.groups * s.kv_heads * p.gtiles * p.gsplit + p.tail * (p.many ? kShWaves : 1) * p.nsplit;
-  if (p.gsplit > 0 || p.tail > 0) x.part = n * (96 + 32 * s.dim) * 4;
+  const int64_t n = s.groups * s.kv_heads * p.gtiles * p.gsplit + p.items * (p.many ? kShWaves : 1) * p.nsplit;
+  if (p.cut) x.part = n * (96 + 32 * s.dim) * 4;
   if (!weigh || heads * s.sq == 0) return x;
   if (p.stored) {
     x.scores = heads * s.sq * s.group() * score_row(s.skv) * 4;
@@ -1198,12 +1192,12 @@ template <int DT, int MODE, int D, bool WEIGH>
 static void launch_shared(const SharedShape& s, hipStream_t stream, const SharedArgs& g) {
   const int64_t heads = s.batch * s.kv_heads;
   const dim3 block(64 * kShWaves);
-  const uint32_t work = g.gwork + g.full + g.tail * (uint32_t)g.nsplit;
+  const uint32_t work = g.gwork + g.items * (uint32_t)g.nsplit;
   hipLaunchKernelGGL((shared_kernel<DT, MODE, D, WEIGH>), dim3(work), block, 0, stream, g);
   const bool stored = WEIGH && g.scores != nullptr;
-  if (g.tail > 0) {
+  if (g.cut) {
     const uint32_t slots = stored ? (uint32_t)((s.skv + kScoreSlots - 1) / kScoreSlots) : 0u;
-    const int64_t rows = g.many ? (int64_t)g.tail * 32 * kShWaves : heads * s.sq * s.group();
+    const int64_t rows = g.many ? (int64_t)g.items * 32 * kShWaves : heads * s.sq * s.group();
     const auto launch = [&](auto teams) {
       constexpr int T = decltype(teams)::value, R = 1024 / D / T;
       const uint32_t joins = (uint32_t)((rows + R - 1) / R);
@@ -1350,6 +1344,7 @@ extern "C" quake_status quake_attention_shared(
   g.gwork = (uint32_t)(p.gitems * p.gsplit);
   g.tiles = (int32_t)p.tiles;
   g.many = p.many;
+  g.cut = p.cut;
   g.nsplit = (int32_t)p.nsplit;
   g.by_group = Div(s.group());
   g.by_sq = Div(sq);
@@ -1358,13 +1353,12 @@ extern "C" quake_status quake_attention_shared(
   g.by_gtiles = Div(p.gmany ? (p.gtiles + kShWaves - 1) / kShWaves : p.gtiles);
   g.by_gsplit = Div(p.gsplit);
   g.by_tiles = Div(p.many ? (p.tiles + kShWaves - 1) / kShWaves : p.tiles);
-  g.by_tail = Div(p.tail);
+  g.by_items = Div(p.items);
   g.by_gper = Div(p.gchunk * (p.gmany ? 1 : 2));
   g.by_per = Div(p.chunk * (p.many ? 1 : 2));
   g.by_rows = Div(p.many ? 32 * kShWaves : sq * s.group());
   g.heads = (uint32_t)(batch * kv_heads);
-  g.full = (uint32_t)p.full;
-  g.tail = (uint32_t)p.tail;
+  g.items = (uint32_t)p.items;
   g.c0 = c0;
   const hipStream_t on = static_cast<hipStream_t>(stream);
   if (dtype == QUAKE_BF16) {

@@ -23,20 +23,18 @@ HARNESS = r"""
 static const char* wrong(const SharedShape& s, bool weigh, bool workspace) {
   const SharedPlan p = shared_plan(s, weigh, workspace);
   const int64_t k31 = (int64_t)1 << 31, k24 = 1 << 24, rows = s.sq * s.group();
-  const int64_t heads = s.batch * s.kv_heads, tail = p.tail;
+  const int64_t heads = s.batch * s.kv_heads, items = heads * wide_tiles(rows, p.many);
   if (p.chunk < 1 || p.chunk * (p.many ? 1 : 2) >= k31) return "keys of a sequence's part";
   if (p.gchunk < 1 || p.gchunk * (p.gmany ? 1 : 2) >= k31) return "keys of a prefix's part";
   if (p.tiles >= k31 || p.gtiles >= k31 || p.nsplit >= k31 || p.gsplit >= k31) return "tiles or parts";
   const int64_t psteps = (s.sp + 63) / 64, steps = (s.skv + 63) / 64 + (p.gsplit > 0 ? 0 : psteps);
   if (p.gsplit > 0 && p.gsplit * p.gchunk < psteps) return "a prefix's keys";
-  if (tail > 0 && p.nsplit * p.chunk < steps) return "a sequence's keys";
-  if (p.gsplit > 0 && tail == 0) return "parts of a group that nothing joins";
-  const int64_t items = heads * wide_tiles(rows, p.many);
-  if (tail != 0 && tail != items) return "tiles of two kinds";
-  const int64_t work = p.gitems * p.gsplit + (tail > 0 ? tail * p.nsplit : items);
-  if (work >= k24) return "workgroups of the tiles";
-  if (tail > 0) {
-    const int64_t joined = p.many ? tail * 128 : heads * rows, slots = p.stored ? (s.skv + 1023) / 1024 : 0;
+  if (p.cut && p.nsplit * p.chunk < steps) return "a sequence's keys";
+  if (p.gsplit > 0 && !p.cut) return "parts of a group that nothing joins";
+  if (p.items != items || (!p.cut && p.nsplit != 1)) return "tiles";
+  if (p.gitems * p.gsplit + items * p.nsplit >= k24) return "workgroups of the tiles";
+  if (p.cut) {
+    const int64_t joined = p.many ? items * 128 : heads * rows, slots = p.stored ? (s.skv + 1023) / 1024 : 0;
     const int64_t team = 1024 / s.dim / (p.gsplit + p.nsplit <= 16 ? 1 : 8);
     if ((joined + team - 1) / team + heads * slots >= k24) return "workgroups of the join";
   }
@@ -75,7 +73,7 @@ int main() {
         }
         const SharedPlan p = shared_plan(s, weigh, workspace);
         ++seen;
-        cut += p.tail > 0;
+        cut += p.cut;
         grouped += p.gsplit > 0;
         stored += p.stored;
       }
