@@ -483,7 +483,8 @@ def quake_attention_shared(q, k, v, prefix_k=None, prefix_v=None, o=None, weight
     held (a new o: undefined). weight: float32 [batch, kv_heads, skv], to which each own key's
     attention weight is added (see quake_cache_evict). t defaults to 1/sqrt(dim); |t q.k|
     below 1e6. `workspace` (from attention_shared_workspace; apart from every operand):
-    without one each sequence reads the prefix for itself; a weight needs one."""
+    without one each sequence reads the prefix for itself; a weight needs one, unless there is
+    no query or no own key."""
     dev, dt = q.get_device(), q.dtype
     for a, what in ((q, "q"), (k, "k"), (v, "v")):
         _operand(a, what, dev)
